@@ -29,7 +29,7 @@
  *     equal scores by smaller token id; NaN ranks below every number.
  *   - The library allocates device memory only in *_create; the hot calls
  *     (ssd_prespeculate, ssd_cache_lookup, ssd_ctx_commit, ssd_verify, ssd_verify_static,
- *     ssd_top_f, ssd_sample) allocate nothing.
+ *     ssd_top_f, ssd_sample, the serving operators) allocate nothing.
  */
 #ifndef SSD_H_
 #define SSD_H_
@@ -342,6 +342,98 @@ int ssd_sample_fp64_scan(const float* d_logits, int64_t ld, const float* d_tempe
 int ssd_sample_split(const float* d_logits, int64_t ld, const float* d_temperature, int32_t rows, int32_t V, uint64_t seed,
                      int32_t row_base, int32_t step, int32_t* d_out, void* d_workspace, int32_t fp64_scan, void* stream);
 size_t ssd_sample_split_workspace_bytes(int32_t rows);
+
+/* ---- serving operators on the caller's own tensors ------------------------------------------------
+ * What a target model of the caller's needs around its matrix products for a step of the loop: rotary positions, the append of
+ * the new keys and values to a paged cache, attention of the new tokens over it, and verification from probabilities.  Stateless,
+ * nothing is allocated, nothing synchronises, every call can be captured into a graph.  Tensors are SSD_F32 or SSD_BF16; sums, softmax
+ * statistics and angles' cosines are fp32 or wider, and what is stored is rounded once.  `*_ld` are elements from a row to the next; the
+ * heads of a row lie one behind the other.  The caller's current device is the one of `stream` and of all buffers. */
+
+/* Rotary positions: the first rot_dim dimensions of a head are rot_dim / 2 pairs, pair (a, b) becomes (a c - b s, b c + a s) with
+ * c = magnitude cos(p f_i), s = magnitude sin(p f_i) at position p; the others pass as they are.  f_i = theta^(-2 i / rot_dim), scaled:
+ *   LINEAR  f_i / factor.
+ *   BANDS   by the turns r = original f_i / 2 pi a pair makes over the `original` context: f_i from `high` turns on, f_i / factor up to
+ *           `low`, between them the two mixed with weight (r - low) / (high - low).
+ *   RAMP    by the pair's index: i(turns) = rot_dim ln(original / (2 pi turns)) / (2 ln theta); f_i up to i0 = floor(i(high)) (at least 0),
+ *           f_i / factor from i1 = ceil(i(low)) (at most rot_dim - 1) on, mixed linearly in i between them. */
+enum { SSD_ROPE_HALF = 0, SSD_ROPE_INTERLEAVED = 1 };                                  /* pairs (i, i + rot_dim / 2), or (2 i, 2 i + 1) */
+enum { SSD_ROPE_PLAIN = 0, SSD_ROPE_LINEAR = 1, SSD_ROPE_BANDS = 2, SSD_ROPE_RAMP = 3 };
+typedef struct {
+  int32_t rot_dim;         /* even, 2..head_dim */
+  int32_t layout, scaling; /* SSD_ROPE_* */
+  float theta;             /* > 1 */
+  float factor;            /* > 0; not read by PLAIN */
+  float low, high;         /* 0 < low < high; BANDS and RAMP */
+  float original;          /* > 0; BANDS and RAMP */
+  float magnitude;         /* > 0; 1 leaves lengths as they are */
+} ssd_rope_config;
+
+/* One layer's keys and values in pages.  Position t of sequence b is position t % page_size of page d_table[b][t / page_size]; KV head h
+ * and dimension d of it are element (page page_stride) + ((t % page_size) n_kv_heads + h) head_dim + d of d_k and d_v.  An entry outside
+ * 0 .. n_pages - 1 names no page: nothing is stored there, and attention does not see its positions.  A call reads the table's entries
+ * of the positions it touches, nothing behind them. */
+typedef struct {
+  void *d_k, *d_v;          /* 16-byte aligned */
+  const int32_t* d_table;   /* [B][table_stride] */
+  int64_t page_stride;      /* elements from a page to the next: page_size n_kv_heads head_dim, or more (keys and values taking turns) */
+  int32_t n_pages;
+  int32_t page_size;        /* a power of two, 8..1024 */
+  int32_t table_stride;
+  int32_t n_kv_heads, head_dim; /* head_dim 64 or 128 */
+  int32_t dtype;
+} ssd_paged_kv;
+
+/* Keys and values that one row alone sees, behind its positions in the pages (a branch's own tokens): [B][T][capacity][n_kv_heads][head_dim]
+ * of the cache's dtype, 16-byte aligned, of which every row sees the first `length`. */
+typedef struct {
+  const void *d_k, *d_v;
+  int32_t capacity;         /* 1..256 */
+  int32_t length;           /* 0..capacity */
+} ssd_tail_kv;
+
+/* d_out[r][h][:] = d_x[r][h][:] at position d_positions[r] (any int32).  head_dim 64 or 128.  In place where d_out and out_ld are d_x and
+ * x_ld; otherwise the two must not overlap. */
+int ssd_rope(const ssd_rope_config* rope, const void* d_x, int64_t x_ld, int32_t dtype, const int32_t* d_positions, int32_t rows,
+             int32_t n_heads, int32_t head_dim, void* d_out, int64_t out_ld, void* stream);
+
+/* Rows [B][T] (row b T + t at d_q + (b T + t) q_ld, likewise the others): queries to d_q_out, rotated keys and the values as they are to
+ * their place in the pages, in the cache's dtype.  d_slots int32 [B][T]: the cache position a row goes to, NULL = its rotary position; a
+ * negative one, one behind the table and one without a page store nothing (rows that only pad).  Two rows of a call must not have the
+ * same place.  In place for the queries as ssd_rope; k and v are only read and must not overlap what is written. */
+int ssd_rope_append(const ssd_rope_config* rope, const ssd_paged_kv* kv, const void* d_q, int64_t q_ld, const void* d_k, int64_t k_ld,
+                    const void* d_v, int64_t v_ld, int32_t dtype, const int32_t* d_positions, const int32_t* d_slots, int32_t B, int32_t T,
+                    int32_t n_q_heads, void* d_q_out, int64_t q_out_ld, void* stream);
+
+/* d_out[b][t][h][:] = sum_j softmax_j(scale q k_j) v_j of KV head h n_kv_heads / n_q_heads (rounded down), j over positions
+ * 0 .. d_visible[b][t] - 1 of sequence b's pages (negative: none; values above max_visible count as max_visible) and the row's tail
+ * (tail NULL: none).  A block of T tokens appended at positions n .. n + T - 1 has visible = n + 1 + t.  A row that sees nothing gives zeros.
+ * What a row does not see does not reach it, whatever is stored there (infinities, NaN).
+ *   dtype        of queries and output; their bases and rows, and the workspace, start on 16 bytes.
+ *   max_visible  host bound of d_visible: sizes the launch, at most table_stride page_size.
+ *   d_lse        float [B][T][n_q_heads] or NULL: ln sum_j exp(scale q k_j), -inf for a row that sees nothing (joins of parts computed elsewhere).
+ *   d_workspace  ssd_paged_attention_workspace_bytes() of device memory for these sizes, private to the call until `stream` has passed it. */
+int ssd_paged_attention(const ssd_paged_kv* kv, const void* d_q, int64_t q_ld, int32_t dtype, const int32_t* d_visible, int32_t B, int32_t T,
+                        int32_t n_q_heads, int32_t max_visible, float scale, const ssd_tail_kv* tail, void* d_out, int64_t out_ld,
+                        float* d_lse, void* d_workspace, void* stream);
+size_t ssd_paged_attention_workspace_bytes(const ssd_paged_kv* kv, int32_t B, int32_t T, int32_t n_q_heads, int32_t max_visible);
+
+/* Verification (Sec. 2.1) from given probabilities and given random numbers: ssd_verify for callers who filter their distributions
+ * (top-p, temperature per request, a grammar) and draw their own numbers.
+ *   d_target_probs [B][K+1][V], d_draft_probs [B][K][V] (rows target_ld and draft_ld apart): row i of a sequence = the distribution of the
+ *   token after s_1..s_i.  They need not sum to one; what is not a positive finite number counts as zero where a token is drawn.
+ *   d_draft_probs NULL: the drafted tokens were certain (a lookup's): q is 1 at s_i and 0 elsewhere.
+ *   d_drafted int32 [B] or NULL (all K): sequence b has its first d_drafted[b] tokens only, kept within 0..K (0: its bonus comes from row 0).
+ *   d_u_accept [B][K], d_u_bonus [B]: uniform in [0,1).
+ * s_{i+1} is accepted while u_i q(s) < p(s), in exact arithmetic; a token outside 0..V-1 is not.  bonus = the first token whose cumulative
+ * mass exceeds u_bonus times the whole, the mass max(p - q, 0) at the first rejected row (p itself where nothing is left of it) and p
+ * behind the last accepted token, summed in fp64; values outside [0,1) are kept within.  A row without mass gives bonus -1.
+ *   out: d_accept_len int32 [B], d_bonus int32 [B].  d_workspace: ssd_verify_probs_workspace_bytes(B, V), 16-byte aligned, private to the
+ *   call until `stream` has passed it.  EINVAL for K outside 1..SSD_MAX_K, V < 2, null pointers. */
+int ssd_verify_probs(const float* d_target_probs, int64_t target_ld, const float* d_draft_probs, int64_t draft_ld, const int32_t* d_spec_tokens,
+                     const int32_t* d_drafted, const float* d_u_accept, const float* d_u_bonus, int32_t B, int32_t K, int32_t V,
+                     int32_t* d_accept_len, int32_t* d_bonus, void* d_workspace, void* stream);
+size_t ssd_verify_probs_workspace_bytes(int32_t B, int32_t V);
 
 /* ---- generic extend (the glue step on its own; also how a target model is run) ------------------ */
 

@@ -22,6 +22,8 @@ SSD_CTX_PER_OPERATOR, SSD_CTX_FUSED_PHASES, SSD_CTX_NARROW_PASSES = 1, 2, 4
 SSD_CTX_ONE_PLANE_ALL = 0x1f00
 SSD_CTX_TWO_PLANES = 0x2000
 SSD_DEBUG_BARRIER_EPOCH, SSD_DEBUG_SPIN_LIMIT = 1, 2
+SSD_ROPE_HALF, SSD_ROPE_INTERLEAVED = 0, 1
+SSD_ROPE_PLAIN, SSD_ROPE_LINEAR, SSD_ROPE_BANDS, SSD_ROPE_RAMP = 0, 1, 2, 3
 
 
 class SsdError(RuntimeError):
@@ -52,6 +54,20 @@ class ssd_views(C.Structure):
                 ("d_glue_hidden", C.c_void_p), ("h_trunk_k", C.POINTER(C.c_void_p)),
                 ("h_trunk_v", C.POINTER(C.c_void_p))] + \
                [(n, C.c_int32) for n in ("batch", "K", "F", "vocab", "d_model", "max_trunk", "fused_pass", "pass_rows")]
+
+
+class ssd_rope_config(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rot_dim", "layout", "scaling")] + \
+               [(n, C.c_float) for n in ("theta", "factor", "low", "high", "original", "magnitude")]
+
+
+class ssd_paged_kv(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_table", C.c_void_p), ("page_stride", C.c_int64)] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "table_stride", "n_kv_heads", "head_dim", "dtype")]
+
+
+class ssd_tail_kv(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("capacity", C.c_int32), ("length", C.c_int32)]
 
 
 EXPORTS = {
@@ -94,6 +110,15 @@ EXPORTS = {
     "ssd_sample_split": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int32, C.c_int32, C.c_uint64, C.c_int32,
                                    C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]),
     "ssd_sample_split_workspace_bytes": (C.c_size_t, [C.c_int32]),
+    "ssd_rope": (C.c_int, [C.POINTER(ssd_rope_config), C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
+                           C.c_void_p, C.c_int64, C.c_void_p]),
+    "ssd_rope_append": (C.c_int, [C.POINTER(ssd_rope_config), C.POINTER(ssd_paged_kv)] + [C.c_void_p, C.c_int64] * 3 +
+                        [C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]),
+    "ssd_paged_attention": (C.c_int, [C.POINTER(ssd_paged_kv), C.c_void_p, C.c_int64, C.c_int32, C.c_void_p] + [C.c_int32] * 4 +
+                            [C.c_float, C.POINTER(ssd_tail_kv), C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "ssd_paged_attention_workspace_bytes": (C.c_size_t, [C.POINTER(ssd_paged_kv)] + [C.c_int32] * 4),
+    "ssd_verify_probs": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64] + [C.c_void_p] * 4 + [C.c_int32] * 3 + [C.c_void_p] * 4),
+    "ssd_verify_probs_workspace_bytes": (C.c_size_t, [C.c_int32, C.c_int32]),
     "ssd_ctx_status": (C.c_int, [C.c_void_p]),
     "ssd_ctx_recover": (C.c_int, [C.c_void_p]),
     "ssd_ctx_debug_set": (C.c_int, [C.c_void_p, C.c_int32, C.c_uint32]),
@@ -370,6 +395,152 @@ def ssd_sample_split(logits: torch.Tensor, temperature: torch.Tensor, seed: int,
 
 def ssd_sample_split_workspace_bytes(rows: int) -> int:
     return int(lib.ssd_sample_split_workspace_bytes(rows))
+
+
+# ---- serving operators on the caller's own tensors
+
+_ROPE_LAYOUTS = {"half": SSD_ROPE_HALF, "interleaved": SSD_ROPE_INTERLEAVED}
+_ROPE_SCALINGS = {"plain": SSD_ROPE_PLAIN, "linear": SSD_ROPE_LINEAR, "bands": SSD_ROPE_BANDS, "ramp": SSD_ROPE_RAMP}
+_DTYPES = {torch.float32: SSD_F32, torch.bfloat16: SSD_BF16}
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _on(device: torch.device, dtype, *tensors: Optional[torch.Tensor]) -> None:
+    """Every tensor is dense, of this type and on this device."""
+    for t in tensors:
+        if t is not None:
+            _need(t.dtype == dtype and t.device == device and t.is_contiguous(), f"a contiguous {dtype} tensor on {device} is needed")
+
+
+def _here(t: torch.Tensor) -> torch.device:
+    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), "the tensors must be on the current GPU")
+    return t.device
+
+
+def _rows(t: torch.Tensor, device: torch.device, dtype: int, what: str) -> int:
+    """Elements from a row of t [..rows..][heads][head_dim] to the next: heads dense, rows evenly spaced."""
+    _need(t.device == device and _DTYPES.get(t.dtype) == dtype, f"{what}: another device or type than the queries")
+    s, n = t.stride(), t.shape
+    _need(s[-1] == 1 and (s[-2] == n[-1] or n[-2] == 1), f"{what}: a row's heads must lie one behind the other")
+    if t.dim() == 4:
+        ld = s[1] if n[1] > 1 else s[0]
+        _need(n[0] <= 1 or n[1] <= 1 or s[0] == n[1] * s[1], f"{what}: rows must be evenly spaced")
+        if n[0] <= 1 and n[1] <= 1:
+            ld = n[-1] * n[-2]
+    else:
+        ld = s[0] if n[0] > 1 else n[-1] * n[-2]
+    _need(ld >= n[-1] * n[-2], f"{what}: rows must not overlap")
+    return ld
+
+
+def rope_config(theta: float, rot_dim: int, layout: str = "half", scaling: str = "plain", factor: float = 1.0, low: float = 0.0,
+                high: float = 0.0, original: float = 0.0, magnitude: float = 1.0) -> ssd_rope_config:
+    return ssd_rope_config(rot_dim, _ROPE_LAYOUTS[layout], _ROPE_SCALINGS[scaling], theta, factor, low, high, original, magnitude)
+
+
+def paged_kv(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor) -> ssd_paged_kv:
+    """One layer's pages [n_pages][page_size][n_kv_heads][head_dim], dense within a page, and the block table int32 [B][blocks].  The
+    result keeps the tensors."""
+    dev = _here(k)
+    _need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.dtype in _DTYPES and v.device == dev,
+          "keys and values must be alike: [n_pages][page_size][n_kv_heads][head_dim], float32 or bfloat16")
+    n, size, heads, d = k.shape
+    _need(n >= 1 and k[0].is_contiguous() and (n == 1 or k.stride(0) >= size * heads * d), "a page must be dense, and pages must not overlap")
+    _need(table.dim() == 2, "block table: int32 [B][blocks]")
+    _on(dev, torch.int32, table)
+    kv = ssd_paged_kv(k.data_ptr(), v.data_ptr(), table.data_ptr(), k.stride(0) if n > 1 else size * heads * d, n, size, table.shape[1],
+                      heads, d, _DTYPES[k.dtype])
+    kv.tensors = (k, v, table)
+    return kv
+
+
+def tail_kv(k: torch.Tensor, v: torch.Tensor, length: int) -> ssd_tail_kv:
+    """Keys and values of single rows [B][T][capacity][n_kv_heads][head_dim], of which the first `length` are seen.  The result keeps the tensors."""
+    _need(k.dim() == 5 and k.shape == v.shape and k.dtype in _DTYPES, "tails: [B][T][capacity][n_kv_heads][head_dim]")
+    _on(_here(k), k.dtype, k, v)
+    tail = ssd_tail_kv(k.data_ptr(), v.data_ptr(), k.shape[2], length)
+    tail.tensors = (k, v)
+    return tail
+
+
+def ssd_rope(rope: ssd_rope_config, x: torch.Tensor, positions: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """x, out [rows][heads][head_dim]; positions int32 [rows]."""
+    dev, dt = _here(x), _DTYPES.get(x.dtype, -1)
+    _need(x.dim() == 3 and out.shape == x.shape and positions.shape == x.shape[:1], "ssd_rope: x and out [rows][heads][head_dim], positions [rows]")
+    _on(dev, torch.int32, positions)
+    rows, heads, d = x.shape
+    _check(lib.ssd_rope(rope, x.data_ptr(), _rows(x, dev, dt, "x"), dt, positions.data_ptr(), rows, heads, d, out.data_ptr(),
+                        _rows(out, dev, dt, "out"), _stream(stream)))
+
+
+def ssd_rope_append(rope: ssd_rope_config, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, kv: ssd_paged_kv,
+                    q_out: torch.Tensor, slots: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q, q_out [B][T][n_q_heads][head_dim]; k, v [B][T][n_kv_heads][head_dim], views of one projection too; positions, slots int32 [B][T]."""
+    dev, dt = _here(q), _DTYPES.get(q.dtype, -1)
+    nb, T, hq, d = q.shape
+    _need(q_out.shape == q.shape and k.shape == (nb, T, kv.n_kv_heads, kv.head_dim) and v.shape == k.shape and d == kv.head_dim,
+          "ssd_rope_append: q and q_out [B][T][n_q_heads][head_dim], k and v [B][T][n_kv_heads][head_dim]")
+    _need(positions.shape == (nb, T) and (slots is None or slots.shape == (nb, T)), "ssd_rope_append: positions and slots [B][T]")
+    _on(dev, torch.int32, positions, slots)
+    _need(kv.tensors[2].shape[0] >= nb and kv.tensors[0].device == dev, "ssd_rope_append: a block table with a row for every sequence, on the queries' device")
+    _check(lib.ssd_rope_append(rope, kv, q.data_ptr(), _rows(q, dev, dt, "q"), k.data_ptr(), _rows(k, dev, dt, "k"), v.data_ptr(),
+                               _rows(v, dev, dt, "v"), dt, positions.data_ptr(), None if slots is None else slots.data_ptr(), nb, T, hq,
+                               q_out.data_ptr(), _rows(q_out, dev, dt, "q_out"), _stream(stream)))
+
+
+def ssd_paged_attention_workspace_bytes(kv: ssd_paged_kv, B: int, T: int, n_q_heads: int, max_visible: int) -> int:
+    return int(lib.ssd_paged_attention_workspace_bytes(kv, B, T, n_q_heads, max_visible))
+
+
+def ssd_paged_attention(kv: ssd_paged_kv, q: torch.Tensor, visible: torch.Tensor, max_visible: int, out: torch.Tensor, workspace: torch.Tensor,
+                        scale: Optional[float] = None, tail: Optional[ssd_tail_kv] = None, lse: Optional[torch.Tensor] = None,
+                        stream=None) -> None:
+    """q, out [B][T][n_q_heads][head_dim]; visible int32 [B][T]; scale None: head_dim ** -0.5; lse float32 [B][T][n_q_heads]."""
+    dev, dt = _here(q), _DTYPES.get(q.dtype, -1)
+    nb, T, hq, d = q.shape
+    _need(out.shape == q.shape and d == kv.head_dim and visible.shape == (nb, T), "ssd_paged_attention: q and out [B][T][n_q_heads][head_dim], visible [B][T]")
+    _on(dev, torch.int32, visible)
+    _need(kv.tensors[2].shape[0] >= nb and kv.tensors[0].device == dev, "ssd_paged_attention: a block table with a row for every sequence, on the queries' device")
+    if lse is not None:
+        _on(dev, torch.float32, lse)
+        _need(lse.shape == (nb, T, hq), "ssd_paged_attention: lse [B][T][n_q_heads]")
+    if tail is not None:
+        tk = tail.tensors[0]
+        _need(tk.shape[:2] == (nb, T) and tk.shape[3:] == (kv.n_kv_heads, d) and tk.dtype == kv.tensors[0].dtype and tk.device == dev,
+              "ssd_paged_attention: tails [B][T][capacity][n_kv_heads][head_dim] of the cache's type")
+    _need(workspace.device == dev and workspace.is_contiguous() and
+          workspace.numel() * workspace.element_size() >= lib.ssd_paged_attention_workspace_bytes(kv, nb, T, hq, max_visible),
+          "ssd_paged_attention: the workspace is too small")
+    _check(lib.ssd_paged_attention(kv, q.data_ptr(), _rows(q, dev, dt, "q"), dt, visible.data_ptr(), nb, T, hq, max_visible,
+                                   d ** -0.5 if scale is None else scale, tail, out.data_ptr(), _rows(out, dev, dt, "out"),
+                                   None if lse is None else lse.data_ptr(), workspace.data_ptr(), _stream(stream)))
+
+
+def ssd_verify_probs_workspace_bytes(B: int, V: int) -> int:
+    return int(lib.ssd_verify_probs_workspace_bytes(B, V))
+
+
+def ssd_verify_probs(target: torch.Tensor, draft: Optional[torch.Tensor], spec_tokens: torch.Tensor, u_accept: torch.Tensor,
+                     u_bonus: torch.Tensor, accept_len: torch.Tensor, bonus: torch.Tensor, workspace: torch.Tensor,
+                     drafted: Optional[torch.Tensor] = None, stream=None) -> None:
+    """target float32 [B][K+1][V], draft float32 [B][K][V] or None (certain tokens); spec_tokens int32 [B][K], u_accept float32 [B][K],
+    u_bonus float32 [B], drafted int32 [B] or None."""
+    dev = _here(target)
+    nb, K1, V = target.shape
+    _on(dev, torch.float32, target, draft, u_accept, u_bonus)
+    _on(dev, torch.int32, spec_tokens, accept_len, bonus, drafted)
+    _need((draft is None or draft.shape == (nb, K1 - 1, V)) and spec_tokens.shape == (nb, K1 - 1) and u_accept.shape == (nb, K1 - 1) and
+          u_bonus.shape == (nb,) and accept_len.shape == (nb,) and bonus.shape == (nb,) and (drafted is None or drafted.shape == (nb,)),
+          "ssd_verify_probs: target [B][K+1][V], draft [B][K][V], spec_tokens and u_accept [B][K], u_bonus, drafted and outputs [B]")
+    _need(workspace.device == dev and workspace.is_contiguous() and
+          workspace.numel() * workspace.element_size() >= lib.ssd_verify_probs_workspace_bytes(nb, V), "ssd_verify_probs: the workspace is too small")
+    _check(lib.ssd_verify_probs(target.data_ptr(), V, None if draft is None else draft.data_ptr(), V, spec_tokens.data_ptr(),
+                                None if drafted is None else drafted.data_ptr(), u_accept.data_ptr(), u_bonus.data_ptr(), nb, K1 - 1, V,
+                                accept_len.data_ptr(), bonus.data_ptr(), workspace.data_ptr(), _stream(stream)))
 
 
 def ssd_ctx_status(ctx: int) -> None:
