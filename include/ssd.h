@@ -371,12 +371,12 @@ typedef struct {
 
 /* One layer's keys and values in pages.  Position t of sequence b is position t % page_size of page d_table[b][t / page_size]; KV head h
  * and dimension d of it are element (page page_stride) + ((t % page_size) n_kv_heads + h) head_dim + d of d_k and d_v.  An entry outside
- * 0 .. n_pages - 1 names no page: nothing is stored there, and attention does not see its positions.  A call reads the table's entries
- * of the positions it touches, nothing behind them. */
+ * 0 .. n_pages - 1 names no page: nothing is stored there, and attention does not see its positions. */
 typedef struct {
   void *d_k, *d_v;          /* 16-byte aligned */
   const int32_t* d_table;   /* [B][table_stride] */
-  int64_t page_stride;      /* elements from a page to the next: page_size n_kv_heads head_dim, or more (keys and values taking turns) */
+  int64_t page_stride;      /* elements from a page to the next: page_size n_kv_heads head_dim, or more (keys and values taking turns),
+                               at most 2^29 and a multiple of 16 bytes */
   int32_t n_pages;
   int32_t page_size;        /* a power of two, 8..1024 */
   int32_t table_stride;

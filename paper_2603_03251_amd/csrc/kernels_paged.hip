@@ -1,18 +1,20 @@
 // Attention of new tokens over a paged key-value cache: o = sum_j softmax_j(scale q k_j) v_j over the positions a row sees, one pass
 // with the running maximum and sum of the softmax, the keys split over blocks where there are few rows and their parts joined.
 //
-// A block serves NQ tiles of 16 query rows (tokens x query heads of one KV head) of one sequence and one split of its positions; its
-// four wavefronts take steps of 32 positions (16 of an fp32 cache) in turn, keys and values straight from memory to the registers
-// that the matrix instructions read.  S^T = K Q^T and O^T = V^T P^T: a query row keeps its lane, and with the keys of the score
-// tiles interleaved a lane ends up with the scores of the 8 (4) consecutive positions that its operand of the second product takes.
-// V^T needs no trip through LDS: a lane loads D / 16 neighbouring dimensions of 8 positions, which one permutation per register turns
-// into D / 16 operands whose row is dimension (lane & 15) D / 16 + e; the output's dimensions are numbered the same way, a lane
-// ends up with 4 D / 16 neighbouring ones.
+// A block serves one or two tiles of 16 query rows (tokens x query heads of one KV head) of one sequence and one split of its positions;
+// its eight wavefronts take steps of 32 positions (16 of an fp32 cache) in turn.  S^T = K Q^T and O^T = V^T P^T: a query row keeps its lane,
+// and the positions of the score tiles are dealt so that a lane ends up with the scores of the 8 (4) positions that its operand of the second
+// product takes.  Keys pass through LDS, straight from memory.  V^T does not: a lane loads D / 16 neighbouring dimensions of its positions, which
+// one permutation per register turns into D / 16 operands whose row is dimension (lane & 15) D / 16 + e; the output's dimensions are numbered
+// the same way, a lane ends up with 4 D / 16 neighbouring ones.
 //
 // Precision: scores, softmax and sums are fp32.  bf16 caches: fp32 queries are three bf16 planes, which is all their 24 bits, and
 // probabilities three too; bf16 queries are their own plane, and probabilities two, 16 bits, where the output keeps 8.
 //
-// What bounds it is the cache's bytes; short ones, the launches and the chain table entry -> keys -> result.
+// What bounds it is the cache's bytes: 64 sequences of 8193 positions, 8 KV heads of 128 dimensions in bf16, 358 us, 6.0 TB/s.  Short ones, the
+// launches, the chain table entry -> keys -> result, and the join: 6 rows x 4102 positions 12.5 us, 3.4 of them the bytes.  Cached, the first
+// takes 78 us: with every lane loading its own row of the keys' operand it took 148, the cache's lines being asked for 2.5 times as often.
+#include <type_traits>
 #include "lanes.h"
 #include "serve.h"
 
@@ -30,74 +32,106 @@ union Bf8 {
   uint32_t w[4];
 };
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 8;
+constexpr int kOwners = 4;              // wavefronts that add the others' parts up
 constexpr int kMaxSplits = 256;
 constexpr int kMaxTail = 256;
 
 struct Parts {          // what a split leaves: [row][query head][split]
-  float* o;             // [D], not divided by the sum
+  float* o;             // [D], not divided by the sum, element e 16 + g 4 + r = dimension (g 4 + r) D / 16 + e
   float2* ml;           // maximum (of scores in powers of two) and sum
   int n_splits, keys_per_split;
 };
 
-template <typename T>
-__device__ __forceinline__ void store4(T* p, f32x4 v) {
-  if constexpr (sizeof(T) == 4) {
-    *(f32x4*)p = v;
-  } else {
-    union { __bf16 e[4]; u32x2 w; } u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) u.e[i] = (__bf16)v[i];
-    *(u32x2*)p = u.w;
-  }
-}
-// four neighbouring dimensions of a row's output
-template <typename TQ>
-__device__ __forceinline__ void store_out(const PagedAttnArgs& a, int64_t row, int head, int d, f32x4 v) {
+// N (1 or 2) neighbouring dimensions of a row's output.
+template <typename TQ, int N>
+__device__ __forceinline__ void store_out(const PagedAttnArgs& a, int64_t row, int head, int d, const float* v) {
   const int64_t at = row * a.out_ld + (int64_t)head * a.head_dim + d;
+  auto put = [&](auto* p, const float* x) {
+    if constexpr (sizeof(*p) == 4) {
+      if constexpr (N == 2) *(float2*)p = make_float2(x[0], x[1]);
+      else *p = x[0];
+    } else {
+      union { __bf16 e[2]; uint32_t w; } u;
+      u.e[0] = (__bf16)x[0];
+      if constexpr (N == 2) {
+        u.e[1] = (__bf16)x[1];
+        *(uint32_t*)p = u.w;
+      } else {
+        *p = (bf16_t)(u.w & 0xffffu);
+      }
+    }
+  };
   if (a.out_plane > 0) {
-    f32x4 rest;
+    float rest[N];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) rest[i] = v[i] - (float)(__bf16)v[i];
-    store4((bf16_t*)a.out + at, v);
-    store4((bf16_t*)a.out + a.out_plane + at, rest);
+    for (int i = 0; i < N; ++i) rest[i] = v[i] - (float)(__bf16)v[i];
+    put((bf16_t*)a.out + at, v);
+    put((bf16_t*)a.out + a.out_plane + at, rest);
   } else {
-    store4((TQ*)a.out + at, v);
+    put((TQ*)a.out + at, v);
   }
 }
 
+__device__ __forceinline__ float lse_of(float m, float l) { return (m + __builtin_amdgcn_logf(l)) * 0.693147180559945f; }
+
+// Two numbers as PLANES bf16 planes each, packed: rounded to the nearest, what is left of it in the next plane.  Three hold all 24 bits.
 template <int PLANES>
-__device__ __forceinline__ void split_planes(float x, __bf16* p, int stride) {
+__device__ __forceinline__ void split_planes(float x, float y, uint32_t* w, int stride) {
+  typedef __attribute__((ext_vector_type(2))) float f32x2;
+  typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 #pragma unroll
   for (int i = 0; i < PLANES; ++i) {
-    p[i * stride] = (__bf16)x;
-    x -= (float)p[i * stride];
+    const uint32_t p = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){x, y}, bf16x2));
+    w[i * stride] = p;
+    x -= __uint_as_float(p << 16);
+    y -= __uint_as_float(p & 0xffff0000u);
   }
 }
 
-// Where a position's keys (or values) of one KV head are, from its table entry: page 0 stands in for an entry that names no page.
-struct Pages {
-  int64_t page_stride, pos_stride;
-  int shift, n_pages;
-  __device__ __forceinline__ bool ok(int page) const { return (unsigned)page < (unsigned)n_pages; }
-  __device__ __forceinline__ int64_t at(int page, int key) const {
-    return (int64_t)(ok(page) ? page : 0) * page_stride + (int64_t)(key & ((1 << shift) - 1)) * pos_stride;
-  }
-};
+__device__ __forceinline__ void load_to_lds(const void* src, uint32_t lds) {     // 16 bytes per lane, to lds + 16 lane
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)(uintptr_t)lds, 16, 0, 0);
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
-template <typename TQ, typename TC, int D, int NQ>
-__global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, Parts parts) {
+// PAGES: table entries of a step: 1 where its positions share a page, else one for every 8.
+template <typename TQ, typename TC, int D, int NQ, int PAGES>
+__global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAttnArgs a, Parts parts) {
   constexpr bool kBf = sizeof(TC) == 2;
   constexpr int KEYS = kBf ? 32 : 16;                    // positions of a wavefront's step
-  constexpr int PER = KEYS / 4;                          // neighbouring ones that a lane holds scores of
+  constexpr int PER = KEYS / 4;                          // of which a lane holds the scores of these: position i 4 + g4, i < PER
   constexpr int VD = D / 16;                             // neighbouring dimensions of a value that a lane loads
   constexpr int QP = sizeof(TQ) == 2 ? 1 : 3, PP = sizeof(TQ) == 2 ? 2 : 3;
-  constexpr int KR = kBf ? 2 * (D / 32) : D / 16;        // 16-byte loads of keys, and of values, per lane and step
-  __shared__ f32x4 mrg[kWaves][VD][64];
-  __shared__ float ml[kWaves][16][2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, li = lane & 15, g4 = lane >> 4;
+  constexpr int ROW = D * sizeof(TC), CH = ROW / 16;     // bytes and 16-byte chunks of a key
+  constexpr int KL = KEYS * ROW / 1024;                  // loads of a step's keys
+  constexpr int VL = PER * (VD * sizeof(TC) > 16 ? 2 : 1), VR = PER * VD * sizeof(TC) / 16;    // of its values, and their registers / 4
+  constexpr int SHARE = KEYS / PAGES;                    // positions that share an entry
+  static_assert(SHARE >= 8, "pages hold 8 positions or more");
+  constexpr int STEP = kWaves * KEYS;
+  constexpr int EW = VD / kOwners;                       // operands of O^T that an owner adds up
+  constexpr int MRG = kOwners * (kWaves - 1) * EW * 1024;
+  static_assert(MRG + kWaves * 128 <= kWaves * KEYS * ROW, "the parts of the wavefronts fit where the keys were");
+  __shared__ __attribute__((aligned(1024))) char lds[kWaves * KEYS * ROW];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), li = lane & 15, g4 = lane >> 4;
   const int hk = blockIdx.x % a.n_kv, split = blockIdx.x / a.n_kv, b = blockIdx.z;
   const int group = a.n_q / a.n_kv, RG = a.T * group, q0 = blockIdx.y * NQ * 16;
+
+  // ---- table entries of a step: the same for all lanes, read ahead of what the rows see (the last block's behind the end of the table)
+  typedef const __attribute__((address_space(4))) int32_t* Table;
+  const Table table = (Table)(uintptr_t)(a.table + (int64_t)b * a.table_stride);
+  const int last_block = max(a.max_visible - 1, 0) >> a.page_shift;
+  struct Entries { int page[PAGES]; };
+  auto entries = [&](int pos) {
+    Entries e;
+#pragma unroll
+    for (int i = 0; i < PAGES; ++i) e.page[i] = table[min((pos + SHARE * i) >> a.page_shift, last_block)];
+    return e;
+  };
+  const int j_begin = split * parts.keys_per_split;
+  int kb = j_begin + wave * KEYS;
+  const Entries first = entries(kb);
+  Entries next = entries(kb + STEP);
 
   // ---- what the rows see
   int vis[NQ], most = 0, least = 0x7fffffff;
@@ -109,19 +143,80 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, P
     most = max(most, vis[n]);
     least = min(least, vis[n]);
   }
-  most = lanes_reduce<8>(most, [](int x, int y) { return max(x, y); });
-  least = lanes_reduce<8>(least, [](int x, int y) { return min(x, y); });
-  const int j_begin = split * parts.keys_per_split, j_end = min(most, j_begin + parts.keys_per_split);
+  most = __builtin_amdgcn_readfirstlane(lanes_reduce<8>(most, [](int x, int y) { return max(x, y); }));
+  least = __builtin_amdgcn_readfirstlane(lanes_reduce<8>(least, [](int x, int y) { return min(x, y); }));
+  const int j_end = min(most, j_begin + parts.keys_per_split);
   // (a split behind the end leaves nothing, and the join does not read it)
   if (split > 0 && j_begin >= j_end) return;
 
-  const Pages pg = {a.page_stride, (int64_t)a.n_kv * D, a.page_shift, a.n_pages};
-  const int32_t* table = a.table + (int64_t)b * a.table_stride;
-  const TC* kbase = (const TC*)a.k + hk * D;
-  const TC* vbase = (const TC*)a.v + hk * D;
+  // ---- where the keys and values of a step are, from its entries; page 0 stands in for an entry that names no page
+  const char* const kbase = (const char*)((const TC*)a.k + hk * D);
+  const char* const vbase = (const char*)((const TC*)a.v + hk * D);
+  const uint32_t page_bytes = (uint32_t)(a.page_stride * sizeof(TC)), pos_bytes = (uint32_t)(a.n_kv * ROW);   // below 2^32: one product reaches any page
+  const int page_mask = (1 << a.page_shift) - 1;
+  struct Place {
+    uint64_t off[PAGES];
+    bool ok[PAGES];
+  };
+  auto place = [&](const Entries& e, int pos) {
+    Place p;
+#pragma unroll
+    for (int i = 0; i < PAGES; ++i) {
+      p.ok[i] = (unsigned)e.page[i] < (unsigned)a.n_pages;
+      p.off[i] = (uint64_t)(uint32_t)(p.ok[i] ? e.page[i] : 0) * page_bytes + (uint32_t)((pos + SHARE * i) & page_mask) * pos_bytes;
+    }
+    return p;
+  };
+  // of the 8 positions from 8 g on
+  auto off_of = [&](const Place& p, int g) { return p.off[g * 8 / SHARE] + (uint32_t)(g * 8 % SHARE) * pos_bytes; };
 
-  // ---- queries, in the order of the second operand of S^T
-  u32x4 qr[NQ][KR / (kBf ? 2 : 1)][kBf ? QP : 1];
+  // Keys go from memory to LDS, a position's row after the other, so that 16 lanes read neighbouring chunks of a row (lanes that loaded
+  // their own row of S^T's operand, 16 rows apart, took the cache 2.5 times as long).  Chunk c of position p is at chunk c ^ swizzle(p),
+  // which puts the 16 rows that an operand is read from on different banks.
+  auto swizzle = [](int p) { return D == 64 && kBf ? ((p >> 1) & 1) * 4 + (p >> 2 & 3) : (p & 3) * 4 + (p >> 2 & 3); };
+  const uint32_t lds_keys = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds + wave * (KEYS * ROW);
+  uint32_t k_off[KL];
+#pragma unroll
+  for (int i = 0; i < KL; ++i) {
+    const int p = i * (64 / CH) + lane / CH;
+    k_off[i] = (p & 7) * pos_bytes + ((lane % CH) ^ swizzle(p)) * 16;
+  }
+  auto load_keys = [&](const Place& p) {
+#pragma unroll
+    for (int i = 0; i < KL; ++i) {
+      load_to_lds(kbase + off_of(p, i * (64 / CH) / 8) + k_off[i], lds_keys + i * 1024);
+    }
+  };
+  u32x4 vr[VR];
+  const uint32_t v_off = g4 * pos_bytes + li * VD * sizeof(TC);
+  auto load_values = [&](const Place& pl) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const char* p = vbase + off_of(pl, j / 2) + (j & 1) * 4 * pos_bytes + v_off;
+      if constexpr (VD * sizeof(TC) == 32) {
+        vr[2 * j] = *(const u32x4*)p;
+        vr[2 * j + 1] = *(const u32x4*)(p + 16);
+      } else if constexpr (VD * sizeof(TC) == 16) {
+        vr[j] = *(const u32x4*)p;
+      } else {
+        const u32x2 w = *(const u32x2*)p;
+        vr[j / 2][(j & 1) * 2] = w[0];
+        vr[j / 2][(j & 1) * 2 + 1] = w[1];
+      }
+    }
+  };
+  Place now = place(first, kb);
+  if (kb < j_end) {
+    load_keys(now);
+    asm volatile("" ::: "memory");                       // the values' loads behind the keys': the loop waits for the older ones only
+    load_values(now);
+  }
+
+  // ---- queries, in the order of the second operand of S^T; a negative scale is theirs
+  const uint32_t sign = a.scale_log2 < 0.f ? 0x8000u : 0u;
+  const float scale = fmaxf(fabsf(a.scale_log2), 1e-37f);     // (0 times the score of a position that is not seen would be no number)
+  auto flip = [&](float x) { return __uint_as_float(__float_as_uint(x) ^ sign << 16); };
+  u32x4 qr[NQ][kBf ? D / 32 : D / 16][kBf ? QP : 1];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     const int qi = min(q0 + n * 16 + li, RG - 1), t = qi / group;
@@ -131,14 +226,15 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, P
       for (int ks = 0; ks < D / 32; ++ks) {
         const TQ* p = src + ks * 32 + g4 * 8;
         if constexpr (QP == 1) {
-          qr[n][ks][0] = *(const u32x4*)p;
+          qr[n][ks][0] = *(const u32x4*)p ^ sign * 0x00010001u;
         } else {
           const f32x4 x0 = *(const f32x4*)p, x1 = *(const f32x4*)(p + 4);
-          union { __bf16 e[QP][8]; u32x4 w[QP]; } u;
+          uint32_t w[QP][4];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) split_planes<QP>(e < 4 ? x0[e & 3] : x1[e & 3], &u.e[0][e], 8);
+          for (int i = 0; i < 4; ++i)
+            split_planes<QP>(flip(i < 2 ? x0[2 * i & 3] : x1[2 * i & 3]), flip(i < 2 ? x0[(2 * i & 3) + 1] : x1[(2 * i & 3) + 1]), &w[0][i], 4);
 #pragma unroll
-          for (int pl = 0; pl < QP; ++pl) qr[n][ks][pl] = u.w[pl];
+          for (int pl = 0; pl < QP; ++pl) qr[n][ks][pl] = (u32x4){w[pl][0], w[pl][1], w[pl][2], w[pl][3]};
         }
       }
     } else {
@@ -146,75 +242,51 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, P
       for (int j = 0; j < D / 16; ++j) {
         const TQ* p = src + j * 16 + g4 * 4;
         if constexpr (sizeof(TQ) == 4) {
-          qr[n][j][0] = *(const u32x4*)p;
+          qr[n][j][0] = *(const u32x4*)p ^ sign << 16;
         } else {
           const u32x2 w = *(const u32x2*)p;
-          qr[n][j][0] = (u32x4){w[0] << 16, w[0] & 0xffff0000u, w[1] << 16, w[1] & 0xffff0000u};
+          qr[n][j][0] = (u32x4){w[0] << 16, w[0] & 0xffff0000u, w[1] << 16, w[1] & 0xffff0000u} ^ sign << 16;
         }
       }
     }
   }
 
   f32x4 acc[NQ][VD];
-  float m_run[NQ], l_run[NQ];
+  // A maximum is renewed when a score exceeds it by 2^kSlack: weights stay below that, and what was added up is seldom scaled again.
+  constexpr float kSlack = 16.f;
+  float m_run[NQ], l_run[NQ], limit[NQ];
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
-    m_run[n] = -INFINITY;
+    m_run[n] = limit[n] = -INFINITY;
     l_run[n] = 0.f;
 #pragma unroll
     for (int e = 0; e < VD; ++e) acc[n][e] = (f32x4){0.f, 0.f, 0.f, 0.f};
   }
 
-  // this lane's keys of a step: bf16, key rows (li >> 2) 8 + tile 4 + (li & 3), so that score register tile 4 + r of lane group g4
-  // is position g4 8 + tile 4 + r; fp32, key row li, register r of group g4 position g4 4 + r.  Neighbouring positions that a lane
-  // takes are on one page (pages hold 8 positions or more), and what is behind j_end is the position before it again, with weight 0.
-  const int krow = kBf ? (li >> 2) * 8 + (li & 3) : li;
-  auto k_entry = [&](int kb) { return table[min(kb + (krow & ~(PER - 1)), j_end - 1) >> a.page_shift]; };
-  auto v_entry = [&](int kb) { return table[min(kb + g4 * PER, j_end - 1) >> a.page_shift]; };
-  int kb = j_begin + wave * KEYS, pk = 0, pv = 0;
-  if (kb < j_end) {
-    pk = k_entry(kb);
-    pv = v_entry(kb);
-  }
-  for (; kb < j_end; kb += kWaves * KEYS) {
-    u32x4 kr[KR], vr[KR];
-    if constexpr (kBf) {
+  // Row li of score tile t is position (t 4 + (li & 3)) 4 + (li >> 2): register r of lane group g4 then is position (t 4 + r) 4 + g4,
+  // and the 4 positions of a load of values, one for each lane group, are neighbours on one page.
+  const int row0 = (li & 3) * 4 + (li >> 2);
+  uint32_t k_at[4];                                      // chunk s 4 + g4 of row li, s < 4 (rows of 32 chunks: the others 256 bytes on)
 #pragma unroll
-      for (int tile = 0; tile < 2; ++tile) {
-        const TC* p = kbase + pg.at(pk, min(kb + krow + tile * 4, j_end - 1)) + g4 * 8;
+  for (int s = 0; s < 4; ++s) k_at[s] = wave * (KEYS * ROW) + row0 * ROW + (((s * 4 + g4) ^ swizzle(row0)) & (CH - 1)) * 16;
+
+  // keys of the next step are requested when this step's scores are taken, its values behind this step's, its table entries one step before
+  for (; kb < j_end; kb += STEP) {
+    const bool more = kb + STEP < j_end;
+    bool pages_ok = true;
 #pragma unroll
-        for (int ks = 0; ks < D / 32; ++ks) kr[tile * (D / 32) + ks] = *(const u32x4*)(p + ks * 32);
-      }
-    } else {
-      const TC* p = kbase + pg.at(pk, min(kb + krow, j_end - 1)) + g4 * 4;
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j) kr[j] = *(const u32x4*)(p + j * 16);
-    }
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const TC* p = vbase + pg.at(pv, min(kb + g4 * PER + j, j_end - 1)) + li * VD;
-      if constexpr (VD * sizeof(TC) == 32) {
-        vr[2 * j] = *(const u32x4*)p;
-        vr[2 * j + 1] = *(const u32x4*)(p + 4);
-      } else if constexpr (VD * sizeof(TC) == 16) {
-        vr[j] = *(const u32x4*)p;
-      } else {
-        const u32x2 w = *(const u32x2*)p;
-        vr[j / 2][(j & 1) * 2] = w[0];
-        vr[j / 2][(j & 1) * 2 + 1] = w[1];
-      }
-    }
-    const bool page_ok = pg.ok(pv);
-    const int pv_now = pv;
-    if (kb + kWaves * KEYS < j_end) {                        // the next step's entries are on their way meanwhile
-      pk = k_entry(kb + kWaves * KEYS);
-      pv = v_entry(kb + kWaves * KEYS);
-    }
+    for (int i = 0; i < PAGES; ++i) pages_ok = pages_ok && now.ok[i];
     // every row sees every position of the step
-    const bool full = kb + KEYS <= min(least, j_end) && __all(page_ok);
+    const bool full = pages_ok && kb + KEYS <= min(least, j_end);
 
     // ---- S^T = K Q^T
     float sv[NQ][PER];
+    wait_loads<VL>();
+    u32x4 kr[KL];
+#pragma unroll
+    for (int t = 0; t < KEYS / 16; ++t)
+#pragma unroll
+      for (int s = 0; s < CH / 4; ++s) kr[t * (CH / 4) + s] = *(const u32x4*)(lds + k_at[s & 3] + t * 16 * ROW + (s >> 2) * 256);
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       if constexpr (kBf) {
@@ -224,42 +296,56 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, P
 #pragma unroll
           for (int ks = 0; ks < D / 32; ++ks)
 #pragma unroll
-            for (int tile = 0; tile < 2; ++tile)
-              S[tile] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[tile * (D / 32) + ks]),
-                                                                __builtin_bit_cast(bf16x8, qr[n][ks][pl]), S[tile], 0, 0, 0);
+            for (int t = 0; t < 2; ++t)
+              S[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[t * (D / 32) + ks]),
+                                                             __builtin_bit_cast(bf16x8, qr[n][ks][pl]), S[t], 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) sv[n][i] = S[i / 4][i & 3] * a.scale_log2;
+        for (int i = 0; i < PER; ++i) sv[n][i] = S[i / 4][i & 3];
       } else {
-        f32x4 S = (f32x4){0.f, 0.f, 0.f, 0.f};
+        f32x4 S[2] = {(f32x4){0.f, 0.f, 0.f, 0.f}, (f32x4){0.f, 0.f, 0.f, 0.f}};   // two chains
 #pragma unroll
         for (int j = 0; j < D / 16; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            S = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[j][e]), __uint_as_float(qr[n][j][0][e]), S, 0, 0, 0);
+            S[e & 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[j][e]), __uint_as_float(qr[n][j][0][e]), S[e & 1], 0, 0, 0);
 #pragma unroll
-        for (int i = 0; i < PER; ++i) sv[n][i] = S[i] * a.scale_log2;
+        for (int i = 0; i < PER; ++i) sv[n][i] = S[0][i] + S[1][i];
       }
     }
+    const Place there = place(next, kb + STEP);
+    if (more) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the keys are read: their place takes the next ones
+      load_keys(there);
+    }
+    next = entries(kb + 2 * STEP);
     bool odd = false;
     if (!full) {
 #pragma unroll
-      for (int n = 0; n < NQ; ++n)
+      for (int i = 0; i < PER; ++i) {
+        const int pos = kb + i * 4 + g4;
+        const bool held = now.ok[i / 2 * 8 / SHARE];
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-          if (!page_ok || kb + g4 * PER + i >= min(vis[n], j_end)) sv[n][i] = -INFINITY;
-      // A row must not feel a position that it does not see, and weight 0 does not keep an infinite or NaN value out of a product:
-      // values that are not finite leave the operand (exponent all ones: the carry out of it lands in the sign bit), and rows that
-      // do see their positions get them added after the product, one by one.
+        for (int n = 0; n < NQ; ++n)
+          if (!held || pos >= min(vis[n], j_end)) sv[n][i] = -INFINITY;
+        // A row must not feel a position that it does not see, and weight 0 does not keep an infinite or NaN value out of a product:
+        // values that no row sees become zeros; among the others those that are not finite leave the operand (exponent all ones: the
+        // carry out of it lands in the sign bit), and rows that do see their positions get them added after the product, one by one.
+        constexpr int RV = VD * sizeof(TC) / 4;              // registers of a position
+        if (!held || pos >= j_end) {
+#pragma unroll
+          for (int x = 0; x < RV; ++x) vr[(i * RV + x) / 4][(i * RV + x) & 3] = 0u;
+        }
+      }
       constexpr uint32_t kExp = kBf ? 0x7f807f80u : 0x7f800000u, kOne = kBf ? 0x00800080u : 0x00800000u;
       uint32_t ones = 0u;
 #pragma unroll
-      for (int j = 0; j < KR; ++j)
+      for (int j = 0; j < VR; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) ones |= (vr[j][i] & kExp) + kOne;
       odd = __any((ones & (kBf ? 0x80008000u : 0x80000000u)) != 0u);
       if (odd) {
 #pragma unroll
-        for (int j = 0; j < KR; ++j)
+        for (int j = 0; j < VR; ++j)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             if constexpr (kBf) {
@@ -271,28 +357,31 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, P
           }
       }
     }
-    // ---- softmax: maximum over the step's positions of a query row (lanes 16 and 32 apart hold the others), weights
-    union { __bf16 e[kBf ? PP : 1][8]; bf16x8 v[kBf ? PP : 1]; } pp[NQ];
+    // ---- softmax: weights 2^(scale (s - max)); lanes 16 and 32 apart hold a query row's other positions
+    uint32_t pw[NQ][kBf ? PP : 1][4];
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
       float mx = sv[n][0];
 #pragma unroll
       for (int i = 1; i < PER; ++i) mx = fmaxf(mx, sv[n][i]);
-      mx = lanes_max<16, 32>(mx);
-      if (__any(mx > m_run[n])) {
-        const float m_new = fmaxf(m_run[n], mx), m_use = m_new == -INFINITY ? 0.f : m_new;
-        const float corr = __builtin_amdgcn_exp2f(m_run[n] - m_use);
-        m_run[n] = m_new;
+      if (__any(mx > limit[n])) {
+        mx = fmaxf(m_run[n], lanes_max<16, 32>(mx));
+        const float corr = m_run[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[n] - mx) * scale);
+        m_run[n] = mx;
+        limit[n] = mx + kSlack / scale;
         l_run[n] *= corr;
 #pragma unroll
         for (int e = 0; e < VD; ++e) acc[n][e] = acc[n][e] * corr;
       }
-      const float m_use = m_run[n] == -INFINITY ? 0.f : m_run[n];
+      const float off = m_run[n] == -INFINITY ? 0.f : -m_run[n] * scale;
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        sv[n][i] = __builtin_amdgcn_exp2f(sv[n][i] - m_use);
+        sv[n][i] = __builtin_amdgcn_exp2f(fmaf(sv[n][i], scale, off));
         l_run[n] += sv[n][i];
-        if constexpr (kBf) split_planes<PP>(sv[n][i], &pp[n].e[0][i], 8);
+      }
+      if constexpr (kBf) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split_planes<PP>(sv[n][2 * i], sv[n][2 * i + 1], &pw[n][0][i], 4);
       }
     }
     // ---- O^T += V^T P^T
@@ -308,7 +397,9 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, P
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
 #pragma unroll
-          for (int pl = PP - 1; pl >= 0; --pl) acc[n][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt.v, pp[n].v[pl], acc[n][e], 0, 0, 0);
+          for (int pl = PP - 1; pl >= 0; --pl)
+            acc[n][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                vt.v, __builtin_bit_cast(bf16x8, (u32x4){pw[n][pl][0], pw[n][pl][1], pw[n][pl][2], pw[n][pl][3]}), acc[n][e], 0, 0, 0);
       } else {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -318,152 +409,236 @@ __global__ __launch_bounds__(256) void paged_attention_kernel(PagedAttnArgs a, P
       }
     }
     if (odd) {
-      for (int gg = 0; gg < 4; ++gg) {
-        const int page = __shfl(pv_now, gg * 16);
+      for (int i = 0; i < KEYS; ++i) {
+        const int pos = kb + i;
+        uint64_t off = now.off[0];
+        bool held = now.ok[0];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-          const int pos = kb + gg * PER + i;
-          if (pos >= j_end || !pg.ok(page)) continue;
-          const TC* vp = vbase + pg.at(page, pos) + g4 * 4 * VD;
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) {
-            const float w = __shfl(sv[n][i], gg * 16 + li);
-            if (pos >= vis[n]) continue;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-              for (int e = 0; e < VD; ++e) {
-                const float x = Elem<TC>::load(vp + r * VD + e);
-                if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) acc[n][e][r] = fmaf(w, x, acc[n][e][r]);
-              }
+        for (int x = 1; x < PAGES; ++x)
+          if (i / SHARE == x) {
+            off = now.off[x];
+            held = now.ok[x];
           }
+        if (pos >= j_end || !held) continue;
+        const TC* vp = (const TC*)(vbase + off + (uint32_t)(i % SHARE) * pos_bytes) + g4 * 4 * VD;
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          float w = sv[n][0];
+#pragma unroll
+          for (int x = 1; x < PER; ++x) w = i / 4 == x ? sv[n][x] : w;
+          w = __shfl(w, (i & 3) * 16 + li);
+          if (pos >= vis[n]) continue;
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < VD; ++e) {
+              const float x = Elem<TC>::load(vp + r * VD + e);
+              if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) acc[n][e][r] = fmaf(w, x, acc[n][e][r]);
+            }
         }
       }
     }
+    if (more) {
+      asm volatile("" ::: "memory");
+      load_values(there);
+    }
+    now = there;
   }
 
-  // ---- the wavefronts' parts meet in LDS: rows, one tile after the other
+  // ---- the wavefronts' parts meet in LDS, one tile of rows after the other; an owner adds up the registers that it holds itself
+  f32x4(*mrg)[kWaves - 1][EW][64] = (f32x4(*)[kWaves - 1][EW][64])lds;
+  float2(*ml)[16] = (float2(*)[16])(lds + MRG);
   const bool last = parts.n_splits == 1 && !a.tail_len;
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     if (q0 + n * 16 >= RG) break;
-    if (n) __syncthreads();
+    __syncthreads();                                         // (the first: keys are no longer read from what follows)
     const float l = lanes_sum<16, 32>(l_run[n]);
+    f32x4 o[EW];
 #pragma unroll
-    for (int e = 0; e < VD; ++e) mrg[wave][e][lane] = acc[n][e];
-    if (g4 == 0) {
-      ml[wave][li][0] = m_run[n];
-      ml[wave][li][1] = l;
-    }
+    for (int w = 0; w < kOwners; ++w)
+#pragma unroll
+      for (int j = 0; j < EW; ++j) {
+        if (wave == w) o[j] = acc[n][w * EW + j];
+        else mrg[w][wave - (wave > w)][j][lane] = acc[n][w * EW + j];
+      }
+    const float m_mine = m_run[n] == -INFINITY ? -INFINITY : m_run[n] * scale;
+    if (g4 == 0) ml[wave][li] = make_float2(m_mine, l);
     __syncthreads();
-    const int qx = threadIdx.x & 15, qi = q0 + n * 16 + qx;
-    float m_all = -INFINITY, l_all = 0.f, wgt[kWaves];
+    const int qi = q0 + n * 16 + li;
+    if (wave >= kOwners) continue;
+    float m_all = -INFINITY, l_all = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m_all = fmaxf(m_all, ml[w][qx][0]);
+    for (int w = 0; w < kWaves; ++w) m_all = fmaxf(m_all, ml[w][li].x);
+    const float m_use = m_all == -INFINITY ? 0.f : m_all, own = __builtin_amdgcn_exp2f(m_mine - m_use);
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      wgt[w] = m_all == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml[w][qx][0] - m_all);
-      l_all += wgt[w] * ml[w][qx][1];
+    for (int w = 0; w < kWaves; ++w) l_all += __builtin_amdgcn_exp2f(ml[w][li].x - m_use) * ml[w][li].y;
+#pragma unroll
+    for (int j = 0; j < EW; ++j) o[j] = o[j] * own;
+#pragma unroll
+    for (int x = 0; x < kWaves - 1; ++x) {
+      const float w = __builtin_amdgcn_exp2f(ml[x + (x >= wave)][li].x - m_use);
+#pragma unroll
+      for (int j = 0; j < EW; ++j) o[j] += mrg[wave][x][j][lane] * w;
     }
     if (qi < RG) {
       const int t = qi / group, head = hk * group + qi - t * group;
       const int64_t row = (int64_t)b * a.T + t, pair = row * a.n_q + head;
-      const float inv = !last ? 1.f : l_all == 0.f ? 0.f : 1.f / l_all;     // a row that sees nothing gives zeros
-      for (int it = threadIdx.x >> 4; it < 4 * VD; it += 16) {
-        const int e4 = it % (VD / 4), r = it / (VD / 4) & 3, gg = it / VD;
-        f32x4 o = (f32x4){0.f, 0.f, 0.f, 0.f};
+      if (last) {
+        const float inv = l_all == 0.f ? 0.f : 1.f / l_all;  // a row that sees nothing gives zeros
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
+        for (int r = 0; r < 4; ++r) {
+          float v[EW];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) o[j] = fmaf(wgt[w], ((const float*)&mrg[w][e4 * 4 + j][qx + 16 * gg])[r], o[j]);
-        o = o * inv;
-        const int d = (gg * 4 + r) * VD + e4 * 4;
-        if (last) store_out<TQ>(a, row, head, d, o);
-        else *(f32x4*)(parts.o + (pair * parts.n_splits + split) * D + d) = o;
-      }
-      if (threadIdx.x < 16) {
-        if (!last) parts.ml[pair * parts.n_splits + split] = make_float2(m_all, l_all);
-        else if (a.lse) a.lse[pair] = (m_all + __builtin_amdgcn_logf(l_all)) * 0.693147180559945f;
+          for (int j = 0; j < EW; ++j) v[j] = o[j][r] * inv;
+          store_out<TQ, EW>(a, row, head, (g4 * 4 + r) * VD + wave * EW, v);
+        }
+        if (a.lse && wave == 0 && g4 == 0) a.lse[pair] = lse_of(m_all, l_all);
+      } else {
+#pragma unroll
+        for (int j = 0; j < EW; ++j) *(f32x4*)(parts.o + (pair * parts.n_splits + split) * D + (wave * EW + j) * 16 + g4 * 4) = o[j];
+        if (wave == 0 && g4 == 0) parts.ml[pair * parts.n_splits + split] = make_float2(m_all, l_all);
       }
     }
   }
 }
 
-// One block per (row, query head): the splits that hold positions of the row, in their order, and the row's tail, which no other row
-// sees and which is a few keys long.
-template <typename TQ, typename TC, int D>
+// WAVES wavefronts per (row, query head): the splits that hold positions of the row, in an order that does not change, and the row's
+// tail, which no other row sees and which is a few keys long.  Everything that does not depend on the row's count of positions is
+// requested before it is known.  A lane holds four elements of a split's part, which are dimensions (g 4 + r) D / 16 + e.
+template <typename TQ, typename TC, int D, int WAVES>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, Parts parts) {
-  constexpr int LD = D / 4, NG = 256 / LD, E = D / 64;
-  __shared__ float w_s[kMaxSplits + kMaxTail];
-  __shared__ float red_m[4], red_l[4];
-  __shared__ f32x4 red_o[NG][LD];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t pair = blockIdx.x, row = pair / a.n_q;
+  constexpr int LD = D / 4, NG = WAVES * 64 / LD, E = D / 64, VD = D / 16, LANES = WAVES * 64, PAIRS = 4 / WAVES;
+  constexpr int AHEAD = 4, OWN = WAVES == 4 ? kMaxSplits / LANES : 1;   // splits a lane requests at once, and whose sums it holds
+  static_assert(OWN == 1, "a lane holds one split's maximum and sum");
+  __shared__ float w_all[PAIRS][LANES + kMaxTail];
+  __shared__ float2 red_ml[4];
+  __shared__ f32x4 red_o[WAVES == 4 ? NG : 1][LD];
+  const int tid = threadIdx.x % LANES, lane = threadIdx.x & 63, wave = tid >> 6;
+  float* w_s = w_all[threadIdx.x / LANES];
+  const int64_t pair = (int64_t)blockIdx.x * PAIRS + threadIdx.x / LANES;
+  if (WAVES == 1 && pair >= (int64_t)a.B * a.T * a.n_q) return;       // no barrier below: a wavefront works by itself
+  auto meet = [] {
+    if constexpr (WAVES == 4) {
+      __syncthreads();
+    } else {
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    }
+  };
+  const int64_t row = pair / a.n_q;
   const int head = (int)(pair - row * a.n_q), hk = head / (a.n_q / a.n_kv);
-  const int vis = min(max(a.visible[row * a.vis_step], 0), a.max_visible);
-  const int n = max(1, (vis + parts.keys_per_split - 1) / parts.keys_per_split), n_all = n + a.tail_len;
+  const int count = a.visible[row * a.vis_step];
+  const float2 own_any = tid < parts.n_splits ? parts.ml[pair * parts.n_splits + tid] : make_float2(-INFINITY, 0.f);
+  const int d4 = tid % LD, gi = tid / LD;
+  const float* po = parts.o + pair * parts.n_splits * D + d4 * 4;
+  f32x4 part[AHEAD];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) part[i] = *(const f32x4*)(po + (int64_t)min(gi + i * NG, parts.n_splits - 1) * D);
+  const int vis = min(max(count, 0), a.max_visible);
+  const int n = max(1, (vis + parts.keys_per_split - 1) / parts.keys_per_split);
+  const float2 own = tid < n ? own_any : make_float2(-INFINITY, 0.f);
   const int64_t tail_ld = (int64_t)a.n_kv * D;
   const TC* tk = (const TC*)a.tail_k + (row * a.tail_cap * a.n_kv + hk) * D;
   const TC* tv = (const TC*)a.tail_v + (row * a.tail_cap * a.n_kv + hk) * D;
-  const float2 own = tid < n ? parts.ml[pair * parts.n_splits + tid] : make_float2(-INFINITY, 0.f);
+  float* t_s = w_s + LANES;
   if (a.tail_len) {
     float q[E];
     const TQ* qp = (const TQ*)a.q + row * a.q_ld + (int64_t)head * D + lane * E;
 #pragma unroll
     for (int e = 0; e < E; ++e) q[e] = Elem<TQ>::load(qp + e);
-    for (int j = wave; j < a.tail_len; j += 4) {
-      float s = 0.f;
+    for (int j0 = wave; j0 < a.tail_len; j0 += WAVES * 8) {
+      float k[8][E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) s = fmaf(q[e], Elem<TC>::load(tk + j * tail_ld + lane * E + e), s);
-      s = lanes_sum(s);
-      if (lane == 0) w_s[kMaxSplits + j] = s * a.scale_log2;
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int e = 0; e < E; ++e) k[i][e] = Elem<TC>::load(tk + min(j0 + i * WAVES, a.tail_len - 1) * tail_ld + lane * E + e);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        float s = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) s = fmaf(q[e], k[i][e], s);
+        s = lanes_sum(s);
+        if (lane == 0 && j0 + i * WAVES < a.tail_len) t_s[j0 + i * WAVES] = s * a.scale_log2;
+      }
     }
-    __syncthreads();
+    meet();
   }
-  const float tail_s = tid < a.tail_len ? w_s[kMaxSplits + tid] : -INFINITY;
-  const float mx = lanes_max(fmaxf(own.x, tail_s));
-  if (lane == 0) red_m[wave] = mx;
-  __syncthreads();
-  const float m_all = fmaxf(fmaxf(red_m[0], red_m[1]), fmaxf(red_m[2], red_m[3])), m_use = m_all == -INFINITY ? 0.f : m_all;
-  const float w = __builtin_amdgcn_exp2f(own.x - m_use), wt = __builtin_amdgcn_exp2f(tail_s - m_use);
+  float mx = own.x;
+  for (int j = tid; j < a.tail_len; j += LANES) mx = fmaxf(mx, t_s[j]);
+  mx = lanes_max(mx);
+  if constexpr (WAVES == 4) {
+    if (lane == 0) red_ml[wave].x = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(red_ml[0].x, red_ml[1].x), fmaxf(red_ml[2].x, red_ml[3].x));
+  }
+  const float m_use = mx == -INFINITY ? 0.f : mx;
+  const float w = __builtin_amdgcn_exp2f(own.x - m_use);
   w_s[tid] = w;
-  if (tid < a.tail_len) w_s[kMaxSplits + tid] = wt;
-  const float ls = lanes_sum(w * own.y + wt);
-  if (lane == 0) red_l[wave] = ls;
-  __syncthreads();
-  const float l_all = (red_l[0] + red_l[1]) + (red_l[2] + red_l[3]);
-  const int d4 = tid % LD, gi = tid / LD;
-  const float* po = parts.o + pair * parts.n_splits * D + d4 * 4;
+  float l = w * own.y;
+  for (int j = tid; j < a.tail_len; j += LANES) {
+    const float wt = __builtin_amdgcn_exp2f(t_s[j] - m_use);
+    t_s[j] = wt;
+    l += wt;
+  }
+  l = lanes_sum(l);
+  if (WAVES == 4 && lane == 0) red_ml[wave].y = l;
+  meet();
+  if constexpr (WAVES == 4) l = (red_ml[0].y + red_ml[1].y) + (red_ml[2].y + red_ml[3].y);
   f32x4 o = (f32x4){0.f, 0.f, 0.f, 0.f};
-  for (int s = gi; s < n; s += NG) o += *(const f32x4*)(po + (int64_t)s * D) * w_s[s];
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (gi + i * NG < n) o += part[i] * w_s[gi + i * NG];
+  for (int s = gi + AHEAD * NG; s < n; s += NG) o += *(const f32x4*)(po + (int64_t)s * D) * w_s[s];
+  // element r of this lane's four is dimension d0 + r VD
+  const int d0 = (d4 & 3) * 4 * VD + (d4 >> 2);
   for (int j = gi; j < a.tail_len; j += NG)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) o[e] = fmaf(w_s[kMaxSplits + j], Elem<TC>::load(tv + j * tail_ld + d4 * 4 + e), o[e]);
-  red_o[gi][d4] = o;
-  __syncthreads();
-  (void)n_all;
-  if (gi == 0) {
+    for (int r = 0; r < 4; ++r) o[r] = fmaf(t_s[j], Elem<TC>::load(tv + j * tail_ld + d0 + r * VD), o[r]);
+  if constexpr (WAVES == 4) {
+    red_o[gi][d4] = o;
+    __syncthreads();
+    if (gi == 0)
 #pragma unroll
-    for (int g = 1; g < NG; ++g) o += red_o[g][d4];
-    store_out<TQ>(a, row, head, d4 * 4, o * (l_all == 0.f ? 0.f : 1.f / l_all));
-    if (d4 == 0 && a.lse) a.lse[pair] = (m_all + __builtin_amdgcn_logf(l_all)) * 0.693147180559945f;
+      for (int g = 1; g < NG; ++g) o += red_o[g][d4];
+  } else if constexpr (LD == 32) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] = lanes_sum<32, 32>(o[r]);
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] = lanes_sum<32, 16>(o[r]);
+  }
+  if (gi == 0) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const float v = o[r] * inv;
+      store_out<TQ, 1>(a, row, head, d0 + r * VD, &v);
+    }
+    if (d4 == 0 && a.lse) a.lse[pair] = lse_of(mx, l);
   }
 }
 
-constexpr int kSplitStep = 128;     // positions: a step of the four wavefronts over a bf16 cache, two over an fp32 cache
+constexpr int kWaveSplits = 16;     // splits up to which one wavefront joins a row
+constexpr int kSplitStep = 256;     // positions: a step of a block's wavefronts over a bf16 cache, two over an fp32 cache
 
 struct Plan {
   int nq, groups, n_splits, keys_per_split;
 };
 
-Plan plan_splits(int B, int T, int n_q, int n_kv, int max_visible) {
+// One tile of 16 query rows to a block, and splits until there are 256 blocks, one for each compute unit: finer ones leave more parts to
+// join than they save (us, 256 / 512 blocks: 6 rows of 64 + 8 heads x 4102 positions of 128 dimensions 12.5 / 15.6, 16 x 6 rows of 32 + 8 heads x up
+// to 2054 of 64 13.8 / 17.8, 1 row of 64 + 8 heads x 32768 31.1 / 37.8).  Two tiles, which read the keys and values once for both, where one each
+// gives two blocks to every unit: 4 x 40 rows of 64 + 8 heads x 8192 122, 156 with one tile; 2 x 300 rows of 32 + 8 heads of 64 dimensions x 2000
+// 38.4, 39.2; not below (6 rows x 4102 15.3, 12.5 with one), and not for fp32 queries, whose planes leave no registers for it.
+Plan plan_splits(int B, int T, int n_q, int n_kv, bool two_tiles, int max_visible) {
   Plan p;
   const int tiles = (int)(((int64_t)T * (n_q / n_kv) + 15) / 16);
-  p.nq = tiles > 2 ? 4 : tiles;
+  p.nq = two_tiles && tiles > 1 && tiles != 3 && (int64_t)B * n_kv * tiles >= 512 ? 2 : 1;
   p.groups = (tiles + p.nq - 1) / p.nq;
   const int64_t units = (int64_t)B * n_kv * p.groups;
   const int steps = max_visible > 0 ? (int)(((int64_t)max_visible + kSplitStep - 1) / kSplitStep) : 1;
-  int64_t n = units < 1024 ? 1024 / units : 1;
+  int64_t n = units < 256 ? 256 / units : 1;
   n = n < steps ? n : steps;
   n = n < kMaxSplits ? n : kMaxSplits;
   const int each = (int)((steps + n - 1) / n);
@@ -474,19 +649,29 @@ Plan plan_splits(int B, int T, int n_q, int n_kv, int max_visible) {
 
 template <typename TQ, typename TC, int D>
 int launch_d(const PagedAttnArgs& a, hipStream_t s) {
-  const Plan p = plan_splits(a.B, a.T, a.n_q, a.n_kv, a.max_visible);
+  constexpr bool kTwoTiles = sizeof(TQ) == 2 && sizeof(TC) == 2;
+  const Plan p = plan_splits(a.B, a.T, a.n_q, a.n_kv, kTwoTiles, a.max_visible);
   Parts parts;
   parts.o = (float*)a.workspace;
   parts.ml = (float2*)(parts.o + (int64_t)a.B * a.T * a.n_q * p.n_splits * D);
   parts.n_splits = p.n_splits;
   parts.keys_per_split = p.keys_per_split;
   const dim3 grid(a.n_kv * p.n_splits, p.groups, a.B);
-  if (p.nq == 1) paged_attention_kernel<TQ, TC, D, 1><<<grid, 256, 0, s>>>(a, parts);
-  else if (p.nq == 2) paged_attention_kernel<TQ, TC, D, 2><<<grid, 256, 0, s>>>(a, parts);
-  else paged_attention_kernel<TQ, TC, D, 4><<<grid, 256, 0, s>>>(a, parts);
+  constexpr int KEYS = sizeof(TC) == 2 ? 32 : 16;
+  auto launch = [&](auto nq) {
+    constexpr int NQ = decltype(nq)::value;
+    if (1 << a.page_shift >= KEYS) paged_attention_kernel<TQ, TC, D, NQ, 1><<<grid, 64 * kWaves, 0, s>>>(a, parts);
+    else paged_attention_kernel<TQ, TC, D, NQ, KEYS / 8><<<grid, 64 * kWaves, 0, s>>>(a, parts);
+  };
+  if constexpr (kTwoTiles) {
+    if (p.nq == 2) launch(std::integral_constant<int, 2>());
+  }
+  if (p.nq == 1) launch(std::integral_constant<int, 1>());
   SSD_HIP(hipGetLastError());
   if (p.n_splits > 1 || a.tail_len) {
-    paged_join_kernel<TQ, TC, D><<<(unsigned)((int64_t)a.B * a.T * a.n_q), 256, 0, s>>>(a, parts);
+    const int64_t pairs = (int64_t)a.B * a.T * a.n_q;
+    if (p.n_splits <= kWaveSplits) paged_join_kernel<TQ, TC, D, 1><<<(unsigned)((pairs + 3) / 4), 256, 0, s>>>(a, parts);
+    else paged_join_kernel<TQ, TC, D, 4><<<(unsigned)pairs, 256, 0, s>>>(a, parts);
     SSD_HIP(hipGetLastError());
   }
   return SSD_OK;
@@ -500,8 +685,10 @@ int launch_types(const PagedAttnArgs& a, hipStream_t s) {
 }  // namespace
 
 size_t paged_attention_workspace(int B, int T, int n_q, int n_kv, int head_dim, int max_visible) {
-  const Plan p = plan_splits(B, T, n_q, n_kv, max_visible);
-  return (size_t)B * T * n_q * p.n_splits * (head_dim + 2) * sizeof(float);
+  // (enough for either type of queries: two tiles a block make more splits)
+  const Plan one = plan_splits(B, T, n_q, n_kv, false, max_visible), two = plan_splits(B, T, n_q, n_kv, true, max_visible);
+  const int n = one.n_splits > two.n_splits ? one.n_splits : two.n_splits;
+  return (size_t)B * T * n_q * n * (head_dim + 2) * sizeof(float);
 }
 
 int launch_paged_attention(int dtype, int cache_dtype, const PagedAttnArgs& a, hipStream_t s) {

@@ -58,8 +58,8 @@ int check_paged_kv(const char* who, const ssd_paged_kv* kv) {
   SSD_CHECK_ARG(kv->n_pages >= 1 && kv->table_stride >= 1, "%s: n_pages and table_stride must be at least 1", who);
   const int per16 = kv->dtype == SSD_BF16 ? 8 : 4;
   SSD_CHECK_ARG(kv->page_stride >= (int64_t)kv->page_size * kv->n_kv_heads * kv->head_dim && kv->page_stride % per16 == 0 &&
-                    kv->page_stride <= INT64_MAX / 8 / kv->n_pages,
-                "%s: page_stride must hold a page and be a multiple of 16 bytes", who);
+                    kv->page_stride <= (1 << 29),
+                "%s: page_stride must hold a page, be a multiple of 16 bytes and at most 2^29", who);
   SSD_CHECK_ARG((((uintptr_t)kv->d_k | (uintptr_t)kv->d_v) & 15) == 0, "%s: the cache must start on 16 bytes", who);
   return SSD_OK;
 }

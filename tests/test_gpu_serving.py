@@ -298,6 +298,25 @@ def test_what_a_row_does_not_see_does_not_reach_it(B, dtype, cache, D):
     assert not torch.isfinite(out[0, 1]).all() and not torch.isfinite(out[0, 3]).all()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_blocks_of_two_tiles(B, D):
+    """Enough rows that a block takes two tiles of them, each row another count of positions; rows whose last positions hold infinities and NaN that
+    the row before does not see; an odd number of tiles; with tails."""
+    g, nb, T, hq, hkv, n = gen(17), 3, 37, 64, 16, 330
+    c = _full_cache(B, g, nb, n, 16, hkv, D, BF16)
+    visible = np.random.default_rng(3).integers(0, n + 1, (nb, T))
+    visible[0] = np.arange(n - T + 1, n + 1)
+    visible[1, :4] = [0, 1, 256, 257]
+    q = randn(g, (nb, T, hq, D), BF16)
+    check_attention(B, c, q, visible, max_visible=n)
+    for j in range(n - 6, n):
+        c.v[c.place(0, j)][j % hkv, j % D] = float("inf") if j % 2 else float("nan")
+    visible[1:] = np.minimum(visible[1:], 40)
+    check_attention(B, c, q, visible, max_visible=n)
+    tk, tv = (randn(g, (nb, T, 3, hkv, D), BF16) for _ in range(2))
+    check_attention(B, c, q, np.minimum(visible, n - 6), tail=(tk, tv, 2), max_visible=n)
+
+
 def test_rows_that_see_nothing(B):
     """Empty slots of a batch, negative counts, tables without a page: zeros, and -inf as the log of the sum; a bound of 0."""
     g = gen(9)
@@ -490,7 +509,7 @@ def test_the_binding_refuses_what_the_kernels_would_read_wrongly(B):
                 lambda: B.paged_kv(c.k[:, :, :, :32], c.v[:, :, :, :32], c.dev_table), lambda: B.paged_kv(c.k.cpu(), c.v.cpu(), c.dev_table),
                 lambda: B.ssd_rope_append(cfg, q, kk.float(), kk, vis, c.kv, q), lambda: B.ssd_rope_append(cfg, q, kk, kk, vis[:, :2], c.kv, q),
                 lambda: B.ssd_rope_append(cfg, q, kk[:, :, :1], kk[:, :, :1], vis, c.kv, q),
-                lambda: B.ssd_rope(cfg, q[0], i32([1, 2]), q[0]), lambda: B.ssd_rope(cfg, q[0].half(), i32([1, 2, 3]), q[0].half()),
+                lambda: B.ssd_rope(cfg, q[0], i32([1, 2]), q[0]), lambda: B.ssd_rope(cfg, q[0].half(), i32([1, 2, 3]), q[0].half()), lambda: B.ssd_rope(cfg, q[0], i32([1, 2, 3]), q[0].float()),
                 lambda: B.ssd_rope(cfg, q[0].expand(3, 4, 64)[:, :1].expand(3, 4, 64), i32([1, 2, 3]), q[0])):
         with pytest.raises(ValueError):
             bad()
