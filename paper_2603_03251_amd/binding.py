@@ -160,7 +160,13 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
     return t.data_ptr()
 
 
+# torch.cuda.current_stream() builds an object: 2.9 us, where asking for the handle takes 0.1
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream: Optional[torch.cuda.Stream]) -> int:
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return (stream or torch.cuda.current_stream()).cuda_stream
 
 
@@ -404,36 +410,43 @@ _ROPE_SCALINGS = {"plain": SSD_ROPE_PLAIN, "linear": SSD_ROPE_LINEAR, "bands": S
 _DTYPES = {torch.float32: SSD_F32, torch.bfloat16: SSD_BF16}
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
+def _bad(what: str):
+    raise ValueError(what)
 
 
-def _on(device: torch.device, dtype, *tensors: Optional[torch.Tensor]) -> None:
-    """Every tensor is dense, of this type and on this device."""
+def _here(t: torch.Tensor) -> int:
+    """The current GPU, which t is on."""
+    dev = t.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        _bad("the tensors must be on the current GPU")
+    return dev
+
+
+def _on(dev: int, dtype, *tensors: Optional[torch.Tensor]) -> None:
+    """Every tensor is dense, of this type and on this GPU."""
     for t in tensors:
-        if t is not None:
-            _need(t.dtype == dtype and t.device == device and t.is_contiguous(), f"a contiguous {dtype} tensor on {device} is needed")
+        if t is not None and not (t.dtype is dtype and t.get_device() == dev and t.is_contiguous()):
+            _bad(f"a contiguous {dtype} tensor on GPU {dev} is needed")
 
 
-def _here(t: torch.Tensor) -> torch.device:
-    _need(t.is_cuda and t.device.index == torch.cuda.current_device(), "the tensors must be on the current GPU")
-    return t.device
-
-
-def _rows(t: torch.Tensor, device: torch.device, dtype: int, what: str) -> int:
+def _rows(t: torch.Tensor, dev: int, dtype) -> int:
     """Elements from a row of t [..rows..][heads][head_dim] to the next: heads dense, rows evenly spaced."""
-    _need(t.device == device and _DTYPES.get(t.dtype) == dtype, f"{what}: another device or type than the queries")
-    s, n = t.stride(), t.shape
-    _need(s[-1] == 1 and (s[-2] == n[-1] or n[-2] == 1), f"{what}: a row's heads must lie one behind the other")
-    if t.dim() == 4:
-        ld = s[1] if n[1] > 1 else s[0]
-        _need(n[0] <= 1 or n[1] <= 1 or s[0] == n[1] * s[1], f"{what}: rows must be evenly spaced")
-        if n[0] <= 1 and n[1] <= 1:
-            ld = n[-1] * n[-2]
+    if t.dtype is not dtype or t.get_device() != dev:
+        _bad("queries, keys, values and outputs must be of one type, on one GPU")
+    n = t.shape
+    if t.is_contiguous():
+        return n[-1] * n[-2]
+    s = t.stride()
+    if s[-1] != 1 or (s[-2] != n[-1] and n[-2] != 1):
+        _bad("a row's heads must lie one behind the other")
+    if len(n) == 4:
+        ld = s[1] if n[1] > 1 else s[0] if n[0] > 1 else n[-1] * n[-2]
+        if n[0] > 1 and n[1] > 1 and s[0] != n[1] * s[1]:
+            _bad("rows must be evenly spaced")
     else:
         ld = s[0] if n[0] > 1 else n[-1] * n[-2]
-    _need(ld >= n[-1] * n[-2], f"{what}: rows must not overlap")
+    if ld < n[-1] * n[-2]:
+        _bad("rows must not overlap")
     return ld
 
 
@@ -446,50 +459,56 @@ def paged_kv(k: torch.Tensor, v: torch.Tensor, table: torch.Tensor) -> ssd_paged
     """One layer's pages [n_pages][page_size][n_kv_heads][head_dim], dense within a page, and the block table int32 [B][blocks].  The
     result keeps the tensors."""
     dev = _here(k)
-    _need(k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.dtype in _DTYPES and v.device == dev,
-          "keys and values must be alike: [n_pages][page_size][n_kv_heads][head_dim], float32 or bfloat16")
+    if not (k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype is v.dtype and k.dtype in _DTYPES and v.get_device() == dev):
+        _bad("keys and values must be alike: [n_pages][page_size][n_kv_heads][head_dim], float32 or bfloat16")
     n, size, heads, d = k.shape
-    _need(n >= 1 and k[0].is_contiguous() and (n == 1 or k.stride(0) >= size * heads * d), "a page must be dense, and pages must not overlap")
-    _need(table.dim() == 2, "block table: int32 [B][blocks]")
+    if not (n >= 1 and k[0].is_contiguous() and (n == 1 or k.stride(0) >= size * heads * d)):
+        _bad("a page must be dense, and pages must not overlap")
+    if table.dim() != 2:
+        _bad("block table: int32 [B][blocks]")
     _on(dev, torch.int32, table)
     kv = ssd_paged_kv(k.data_ptr(), v.data_ptr(), table.data_ptr(), k.stride(0) if n > 1 else size * heads * d, n, size, table.shape[1],
                       heads, d, _DTYPES[k.dtype])
-    kv.tensors = (k, v, table)
+    kv.tensors, kv.device, kv.sequences = (k, v, table), dev, table.shape[0]
     return kv
 
 
 def tail_kv(k: torch.Tensor, v: torch.Tensor, length: int) -> ssd_tail_kv:
     """Keys and values of single rows [B][T][capacity][n_kv_heads][head_dim], of which the first `length` are seen.  The result keeps the tensors."""
-    _need(k.dim() == 5 and k.shape == v.shape and k.dtype in _DTYPES, "tails: [B][T][capacity][n_kv_heads][head_dim]")
+    if not (k.dim() == 5 and k.shape == v.shape and k.dtype in _DTYPES):
+        _bad("tails: [B][T][capacity][n_kv_heads][head_dim], float32 or bfloat16")
     _on(_here(k), k.dtype, k, v)
     tail = ssd_tail_kv(k.data_ptr(), v.data_ptr(), k.shape[2], length)
-    tail.tensors = (k, v)
+    tail.tensors, tail.like = (k, v), (k.get_device(), k.dtype, tuple(k.shape[:2]) + tuple(k.shape[3:]))
     return tail
 
 
 def ssd_rope(rope: ssd_rope_config, x: torch.Tensor, positions: torch.Tensor, out: torch.Tensor, stream=None) -> None:
     """x, out [rows][heads][head_dim]; positions int32 [rows]."""
-    dev, dt = _here(x), _DTYPES.get(x.dtype, -1)
-    _need(x.dim() == 3 and out.shape == x.shape and positions.shape == x.shape[:1], "ssd_rope: x and out [rows][heads][head_dim], positions [rows]")
+    dev, dt = _here(x), x.dtype
+    shape = x.shape
+    if len(shape) != 3 or out.shape != shape or positions.shape != shape[:1] or dt not in _DTYPES:
+        _bad("ssd_rope: x and out [rows][heads][head_dim], float32 or bfloat16, and positions [rows]")
     _on(dev, torch.int32, positions)
-    rows, heads, d = x.shape
-    _check(lib.ssd_rope(rope, x.data_ptr(), _rows(x, dev, dt, "x"), dt, positions.data_ptr(), rows, heads, d, out.data_ptr(),
-                        _rows(out, dev, dt, "out"), _stream(stream)))
+    _check(lib.ssd_rope(rope, x.data_ptr(), _rows(x, dev, dt), _DTYPES[dt], positions.data_ptr(), shape[0], shape[1], shape[2], out.data_ptr(),
+                        _rows(out, dev, dt), _stream(stream)))
 
 
 def ssd_rope_append(rope: ssd_rope_config, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, kv: ssd_paged_kv,
                     q_out: torch.Tensor, slots: Optional[torch.Tensor] = None, stream=None) -> None:
     """q, q_out [B][T][n_q_heads][head_dim]; k, v [B][T][n_kv_heads][head_dim], views of one projection too; positions, slots int32 [B][T]."""
-    dev, dt = _here(q), _DTYPES.get(q.dtype, -1)
+    dev, dt = _here(q), q.dtype
     nb, T, hq, d = q.shape
-    _need(q_out.shape == q.shape and k.shape == (nb, T, kv.n_kv_heads, kv.head_dim) and v.shape == k.shape and d == kv.head_dim,
-          "ssd_rope_append: q and q_out [B][T][n_q_heads][head_dim], k and v [B][T][n_kv_heads][head_dim]")
-    _need(positions.shape == (nb, T) and (slots is None or slots.shape == (nb, T)), "ssd_rope_append: positions and slots [B][T]")
+    if q_out.shape != q.shape or k.shape != (nb, T, kv.n_kv_heads, kv.head_dim) or v.shape != k.shape or d != kv.head_dim or dt not in _DTYPES:
+        _bad("ssd_rope_append: q and q_out [B][T][n_q_heads][head_dim], k and v [B][T][n_kv_heads][head_dim], float32 or bfloat16")
+    if positions.shape != (nb, T) or (slots is not None and slots.shape != (nb, T)):
+        _bad("ssd_rope_append: positions and slots [B][T]")
     _on(dev, torch.int32, positions, slots)
-    _need(kv.tensors[2].shape[0] >= nb and kv.tensors[0].device == dev, "ssd_rope_append: a block table with a row for every sequence, on the queries' device")
-    _check(lib.ssd_rope_append(rope, kv, q.data_ptr(), _rows(q, dev, dt, "q"), k.data_ptr(), _rows(k, dev, dt, "k"), v.data_ptr(),
-                               _rows(v, dev, dt, "v"), dt, positions.data_ptr(), None if slots is None else slots.data_ptr(), nb, T, hq,
-                               q_out.data_ptr(), _rows(q_out, dev, dt, "q_out"), _stream(stream)))
+    if kv.sequences < nb or kv.device != dev:
+        _bad("ssd_rope_append: a block table with a row for every sequence, on the queries' GPU")
+    _check(lib.ssd_rope_append(rope, kv, q.data_ptr(), _rows(q, dev, dt), k.data_ptr(), _rows(k, dev, dt), v.data_ptr(), _rows(v, dev, dt), _DTYPES[dt],
+                               positions.data_ptr(), None if slots is None else slots.data_ptr(), nb, T, hq, q_out.data_ptr(),
+                               _rows(q_out, dev, dt), _stream(stream)))
 
 
 def ssd_paged_attention_workspace_bytes(kv: ssd_paged_kv, B: int, T: int, n_q_heads: int, max_visible: int) -> int:
@@ -500,23 +519,24 @@ def ssd_paged_attention(kv: ssd_paged_kv, q: torch.Tensor, visible: torch.Tensor
                         scale: Optional[float] = None, tail: Optional[ssd_tail_kv] = None, lse: Optional[torch.Tensor] = None,
                         stream=None) -> None:
     """q, out [B][T][n_q_heads][head_dim]; visible int32 [B][T]; scale None: head_dim ** -0.5; lse float32 [B][T][n_q_heads]."""
-    dev, dt = _here(q), _DTYPES.get(q.dtype, -1)
+    dev, dt = _here(q), q.dtype
     nb, T, hq, d = q.shape
-    _need(out.shape == q.shape and d == kv.head_dim and visible.shape == (nb, T), "ssd_paged_attention: q and out [B][T][n_q_heads][head_dim], visible [B][T]")
+    if out.shape != q.shape or d != kv.head_dim or visible.shape != (nb, T) or dt not in _DTYPES:
+        _bad("ssd_paged_attention: q and out [B][T][n_q_heads][head_dim], float32 or bfloat16, and visible [B][T]")
     _on(dev, torch.int32, visible)
-    _need(kv.tensors[2].shape[0] >= nb and kv.tensors[0].device == dev, "ssd_paged_attention: a block table with a row for every sequence, on the queries' device")
+    if kv.sequences < nb or kv.device != dev:
+        _bad("ssd_paged_attention: a block table with a row for every sequence, on the queries' GPU")
     if lse is not None:
         _on(dev, torch.float32, lse)
-        _need(lse.shape == (nb, T, hq), "ssd_paged_attention: lse [B][T][n_q_heads]")
-    if tail is not None:
-        tk = tail.tensors[0]
-        _need(tk.shape[:2] == (nb, T) and tk.shape[3:] == (kv.n_kv_heads, d) and tk.dtype == kv.tensors[0].dtype and tk.device == dev,
-              "ssd_paged_attention: tails [B][T][capacity][n_kv_heads][head_dim] of the cache's type")
-    _need(workspace.device == dev and workspace.is_contiguous() and
-          workspace.numel() * workspace.element_size() >= lib.ssd_paged_attention_workspace_bytes(kv, nb, T, hq, max_visible),
-          "ssd_paged_attention: the workspace is too small")
-    _check(lib.ssd_paged_attention(kv, q.data_ptr(), _rows(q, dev, dt, "q"), dt, visible.data_ptr(), nb, T, hq, max_visible,
-                                   d ** -0.5 if scale is None else scale, tail, out.data_ptr(), _rows(out, dev, dt, "out"),
+        if lse.shape != (nb, T, hq):
+            _bad("ssd_paged_attention: lse [B][T][n_q_heads]")
+    if tail is not None and tail.like != (dev, kv.tensors[0].dtype, (nb, T, kv.n_kv_heads, d)):
+        _bad("ssd_paged_attention: tails [B][T][capacity][n_kv_heads][head_dim] of the cache's type")
+    if workspace.get_device() != dev or not workspace.is_contiguous() or \
+            workspace.nbytes < lib.ssd_paged_attention_workspace_bytes(kv, nb, T, hq, max_visible):
+        _bad("ssd_paged_attention: the workspace is too small")
+    _check(lib.ssd_paged_attention(kv, q.data_ptr(), _rows(q, dev, dt), _DTYPES[dt], visible.data_ptr(), nb, T, hq, max_visible,
+                                   d ** -0.5 if scale is None else scale, tail, out.data_ptr(), _rows(out, dev, dt),
                                    None if lse is None else lse.data_ptr(), workspace.data_ptr(), _stream(stream)))
 
 
@@ -533,11 +553,12 @@ def ssd_verify_probs(target: torch.Tensor, draft: Optional[torch.Tensor], spec_t
     nb, K1, V = target.shape
     _on(dev, torch.float32, target, draft, u_accept, u_bonus)
     _on(dev, torch.int32, spec_tokens, accept_len, bonus, drafted)
-    _need((draft is None or draft.shape == (nb, K1 - 1, V)) and spec_tokens.shape == (nb, K1 - 1) and u_accept.shape == (nb, K1 - 1) and
-          u_bonus.shape == (nb,) and accept_len.shape == (nb,) and bonus.shape == (nb,) and (drafted is None or drafted.shape == (nb,)),
-          "ssd_verify_probs: target [B][K+1][V], draft [B][K][V], spec_tokens and u_accept [B][K], u_bonus, drafted and outputs [B]")
-    _need(workspace.device == dev and workspace.is_contiguous() and
-          workspace.numel() * workspace.element_size() >= lib.ssd_verify_probs_workspace_bytes(nb, V), "ssd_verify_probs: the workspace is too small")
+    one, each = (nb,), (nb, K1 - 1)
+    if (draft is not None and draft.shape != (nb, K1 - 1, V)) or spec_tokens.shape != each or u_accept.shape != each or u_bonus.shape != one or \
+            accept_len.shape != one or bonus.shape != one or (drafted is not None and drafted.shape != one):
+        _bad("ssd_verify_probs: target [B][K+1][V], draft [B][K][V], spec_tokens and u_accept [B][K], u_bonus, drafted and outputs [B]")
+    if workspace.get_device() != dev or not workspace.is_contiguous() or workspace.nbytes < lib.ssd_verify_probs_workspace_bytes(nb, V):
+        _bad("ssd_verify_probs: the workspace is too small")
     _check(lib.ssd_verify_probs(target.data_ptr(), V, None if draft is None else draft.data_ptr(), V, spec_tokens.data_ptr(),
                                 None if drafted is None else drafted.data_ptr(), u_accept.data_ptr(), u_bonus.data_ptr(), nb, K1 - 1, V,
                                 accept_len.data_ptr(), bonus.data_ptr(), workspace.data_ptr(), _stream(stream)))
