@@ -98,8 +98,11 @@ typedef struct {
   int32_t kv_pages;  /* 0: every sequence owns max_trunk trunk positions.  n >= 2: paged trunk (App. B, the paged attention and
                         block tables of the paper's system): per layer one pool of n pages of 32 positions, shared by the
                         sequences, each reaching its positions through its row of a block table; page 0 is the all-zero
-                        page every unmapped block points at and is never handed out.  Fused contexts only, max_trunk <=
-                        16384 (it then only sizes the block table).  Same bits as the contiguous trunk. */
+                        page every unmapped block points at and is never handed out.  max_trunk then only sizes the block
+                        table (contexts of fused passes: <= 16384).  Contexts of fused passes give the same bits as with the
+                        contiguous trunk.  Contexts of models that the fused passes do not take (fp32, head_dim 128) run
+                        the serving operators below over their pages: the same to rounding.  EINVAL with SSD_CTX_PER_OPERATOR,
+                        which asks for the kernels of the contiguous trunk. */
 } ssd_round_config;
 
 /* ssd_round_config.flags.  By default a context whose model and shape the fused decode pass supports (bf16, head_dim 64)
@@ -171,6 +174,11 @@ int ssd_model_create(const ssd_model_config* cfg, const ssd_model_weights* w, vo
  * 4 w_gate, 5 w_up, 6 w_down} for layer l.  Runs on `stream` and SYNCHRONISES it before returning. */
 int ssd_model_create_random(const ssd_model_config* cfg, uint64_t seed, void* stream, ssd_model** out);
 int ssd_model_destroy(ssd_model* m);
+/* Rotary positions of the model's heads, in place of the configuration's plain rope_theta (a context longer than the one the
+ * model was first trained on): scaling, theta and magnitude as ssd_rope_config has them below; whole heads in pairs
+ * (i, i + head_dim / 2), so rot_dim has to be head_dim and layout SSD_ROPE_HALF.  To be called before the contexts that are to use it run. */
+struct ssd_rope_config;
+int ssd_model_set_rope(ssd_model* m, const struct ssd_rope_config* rope);
 /* A bf16 model whose shape the fused passes take holds every linear layer twice: in the order the fused passes stream
  * it, and in the tile order of the per-operator kernels (contexts with SSD_CTX_PER_OPERATOR, or round shapes the fused
  * passes do not take).  A caller that only creates fused contexts gives the second copy back (2.47 GB at the 1B shape):
@@ -359,7 +367,7 @@ size_t ssd_sample_split_workspace_bytes(int32_t rows);
  *           f_i / factor from i1 = ceil(i(low)) (at most rot_dim - 1) on, mixed linearly in i between them. */
 enum { SSD_ROPE_HALF = 0, SSD_ROPE_INTERLEAVED = 1 };                                  /* pairs (i, i + rot_dim / 2), or (2 i, 2 i + 1) */
 enum { SSD_ROPE_PLAIN = 0, SSD_ROPE_LINEAR = 1, SSD_ROPE_BANDS = 2, SSD_ROPE_RAMP = 3 };
-typedef struct {
+typedef struct ssd_rope_config {
   int32_t rot_dim;         /* even, 2..head_dim */
   int32_t layout, scaling; /* SSD_ROPE_* */
   float theta;             /* > 1 */

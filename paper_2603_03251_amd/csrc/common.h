@@ -93,6 +93,20 @@ struct Dims {
   int qkv_dim() const { return q_dim() + 2 * kv_dim(); }
 };
 
+// How a model's rotary frequencies are scaled (ssd_rope_config): the factor of pair i, which makes `turns` turns per position.
+struct RopeScaling {
+  int kind;              // SSD_ROPE_PLAIN ..
+  float factor, low, high, original, magnitude;
+  float i0, i1;          // RAMP: the pairs between which it falls
+};
+__host__ __device__ __forceinline__ double rope_share(const RopeScaling& r, double turns, int i) {
+  double keep = 0.0;
+  if (r.kind == SSD_ROPE_BANDS) keep = (r.original * turns - r.low) / ((double)r.high - r.low);
+  if (r.kind == SSD_ROPE_RAMP) keep = 1.0 - (i - (double)r.i0) / fmax((double)r.i1 - r.i0, 1e-3);
+  keep = fmin(fmax(keep, 0.0), 1.0);
+  return r.kind == SSD_ROPE_PLAIN ? 1.0 : keep + (1.0 - keep) / r.factor;
+}
+
 // Cache shape (Sec. 4.1.2): fan-out per accept length as running offsets.  Accept length k owns the F_k =
 // off[k+1] - off[k] consecutive branch rows off[k] .. off[k+1]-1 of its sequence; off[K+1] is the rows per sequence.
 // The uniform shape is off[k] = k F.  Passed to kernels by value.
@@ -111,11 +125,12 @@ struct EmbedGather {
 // Row descriptors + rotary tables for a branch step / an extend, from device-side trunk lengths.  The branch version
 // also gathers the token every row feeds at this step into step_tokens (null: skipped).
 int launch_setup_branch_rows(RowDesc* rows, float* cos_sin, const int32_t* trunk_len, int B, int K, const FanTable& fan, int step,
-                             int half_dim, float theta, int32_t* step_tokens, const int32_t* keys,
+                             int half_dim, float theta, const RopeScaling& scaling, int32_t* step_tokens, const int32_t* keys,
                              const int32_t* cache_tokens, const int32_t* forced_keys, const int32_t* forced_tokens,
                              const EmbedGather& embed, hipStream_t s);
 int launch_setup_extend_rows(RowDesc* rows, float* cos_sin, const int32_t* trunk_len, const int32_t* limit, int B, int T, int offset,
-                             int half_dim, float theta, int seq_base, const EmbedGather& embed, const int32_t* tokens, hipStream_t s);
+                             int half_dim, float theta, const RopeScaling& scaling, int seq_base, const EmbedGather& embed,
+                             const int32_t* tokens, hipStream_t s);
 int launch_rmsnorm(int dtype, const float* h, const void* gain, void* xn, int64_t xn_plane, float* copy_out,
                    int64_t copy_ld, int M, int d, float eps, hipStream_t s);
 // bf16 models: rotary embedding of q and k (fp32 [M][qkv_dim]) + write of q (fp32) and of the row's K/V into the trunk or
@@ -129,7 +144,9 @@ int launch_lookup(const int32_t* keys, const int32_t* cache_tokens, const float*
                   const int32_t* bonus, uint8_t* hit, int32_t* branch, int32_t* spec, const float** logits_ptr, int B,
                   int K, const FanTable& fan, int V, hipStream_t s);
 int launch_pending_exclude(int32_t* exclude, const int32_t* pending, int B, int K, hipStream_t s);
-int launch_copy_kv_in(int dtype, void* trunk, const void* src, int B, int len, int max_trunk, int row_elems, hipStream_t s);
+// pages (or null): block j of sequence b is page pages[b page_stride + j] of 32 positions
+int launch_copy_kv_in(int dtype, void* trunk, const void* src, int B, int len, int max_trunk, int row_elems, const int32_t* pages,
+                      int page_stride, hipStream_t s);
 
 // ---------------------------------------------------------------- kernels_init.hip
 // Seeded synthetic tensors generated on the device (bit-identical to the host-side input generators' twin).

@@ -39,7 +39,8 @@ __global__ void fill_const_kernel(T* __restrict__ dst, int64_t n, float v) {
 // Synthetic trunk KV of one layer: element (b, pos, kv head h, dim d), pos < len[b], has index
 // (b << 40) + (pos Hkv + h) D + d in tensor `id_k` / `id_v`.  fused != 0: the head-major layouts of the fused pass (keys
 // [B][Hkv][stride][64], values transposed per 32-position block), or with pages != null their paged form (block j of
-// sequence b in page pages[b * page_stride + j] of a pool [page][Hkv][..]); else [B][stride][Hkv][D].
+// sequence b in page pages[b * page_stride + j] of a pool [page][Hkv][..]); else [B][stride][Hkv][D], or with pages != null
+// [page][32][Hkv][D].
 template <typename T>
 __global__ void fill_kv_kernel(T* __restrict__ k, T* __restrict__ v, const int32_t* __restrict__ len, int B, int max_len, int Hkv,
                                int D, int stride, int fused, const int32_t* __restrict__ pages, int page_stride,
@@ -60,7 +61,8 @@ __global__ void fill_kv_kernel(T* __restrict__ k, T* __restrict__ v, const int32
     Elem<T>::store(k + bb + (int64_t)(pos & 31) * 64 + d, kv);
     Elem<T>::store(v + bb + d * 32 + (pos & 31), vv);
   } else {
-    const int64_t at = (((int64_t)b * stride + pos) * Hkv + h) * D + d;
+    const int64_t slot = pages ? (int64_t)pages[b * page_stride + (pos >> 5)] * 32 + (pos & 31) : (int64_t)b * stride + pos;
+    const int64_t at = (slot * Hkv + h) * D + d;
     Elem<T>::store(k + at, kv);
     Elem<T>::store(v + at, vv);
   }

@@ -9,13 +9,14 @@ namespace {
 
 constexpr int kBlock = 256;
 
-// Rotary table entry for (row, i): cos and sin of pos * theta^(-2i/D), evaluated in fp64.
-__device__ __forceinline__ void write_cos_sin(float* cos_sin, int row, int half_dim, int i, int pos, float theta) {
+// Rotary table entry for (row, i): cos and sin of pos * theta^(-2i/D), scaled, evaluated in fp64.
+__device__ __forceinline__ void write_cos_sin(float* cos_sin, int row, int half_dim, int i, int pos, float theta, const RopeScaling& scaling) {
   double inv = pow((double)theta, -2.0 * (double)i / (double)(2 * half_dim));
+  if (scaling.kind != SSD_ROPE_PLAIN) inv *= rope_share(scaling, inv / 6.283185307179586476925, i);
   double ang = (double)pos * inv;
   double sn, cs;
   sincos(ang, &sn, &cs);
-  *(float2*)(cos_sin + ((int64_t)row * half_dim + i) * 2) = make_float2((float)cs, (float)sn);
+  *(float2*)(cos_sin + ((int64_t)row * half_dim + i) * 2) = make_float2((float)cs * scaling.magnitude, (float)sn * scaling.magnitude);
 }
 
 // Block `block` of an embedding gather: kBlock x 4 elements of a row (d is a multiple of 4).
@@ -42,7 +43,7 @@ __device__ __forceinline__ void embed_part(const EmbedGather& e, int m, int part
 // of step `step`, and the token every row feeds (its cache key at step 0, afterwards the token it drew one step
 // earlier; the forced arrays replace both under teacher forcing).
 __global__ void setup_branch_rows_kernel(RowDesc* rows, float* cos_sin, const int32_t* trunk_len, int M, int K,
-                                         FanTable fan, int step, int half_dim, float theta, int32_t* step_tokens, const int32_t* keys,
+                                         FanTable fan, int step, int half_dim, float theta, RopeScaling scaling, int32_t* step_tokens, const int32_t* keys,
                                          const int32_t* cache_tokens, const int32_t* forced_keys,
                                          const int32_t* forced_tokens, EmbedGather embed, int setup_blocks) {
   auto token_of = [&](int m) {
@@ -69,14 +70,14 @@ __global__ void setup_branch_rows_kernel(RowDesc* rows, float* cos_sin, const in
     rows[m] = r;
     if (step_tokens) step_tokens[m] = token_of(m);
   }
-  write_cos_sin(cos_sin, m, half_dim, i, pos, theta);
+  write_cos_sin(cos_sin, m, half_dim, i, pos, theta, scaling);
 }
 
 // Extend rows: token t of sequence b at position trunk_len+offset+t, causal (sees itself after the append).
 // rows of sequences seq_base .. seq_base + B - 1 (row m of the pass = token m % T of sequence seq_base + m / T)
 // limit (or null): sequence b stores the keys of its first limit[b] trunk positions only, rows behind them pad
 __global__ void setup_extend_rows_kernel(RowDesc* rows, float* cos_sin, const int32_t* trunk_len, const int32_t* limit, int B, int T,
-                                         int offset, int half_dim, float theta, int seq_base, EmbedGather embed,
+                                         int offset, int half_dim, float theta, RopeScaling scaling, int seq_base, EmbedGather embed,
                                          const int32_t* tokens, int setup_blocks) {
   if ((int)blockIdx.x >= setup_blocks) {                       // blocks behind the set-up's: the embedding gather
     const int part = (int)blockIdx.x - setup_blocks, per_row = embed_blocks_per_row(embed.d);
@@ -94,7 +95,7 @@ __global__ void setup_extend_rows_kernel(RowDesc* rows, float* cos_sin, const in
     r.kv_slot = limit && pos >= limit[b] ? -1 : pos;
     rows[m] = r;
   }
-  write_cos_sin(cos_sin, m, half_dim, i, pos, theta);
+  write_cos_sin(cos_sin, m, half_dim, i, pos, theta, scaling);
 }
 
 __device__ __forceinline__ float block_sum(float v, float* smem) {
@@ -272,12 +273,18 @@ __global__ void pending_exclude_kernel(int32_t* exclude, const int32_t* pending,
 }
 
 template <typename T>
-__global__ void copy_kv_in_kernel(T* trunk, const T* src, int len, int max_trunk, int row_elems, int64_t total) {
+__global__ void copy_kv_in_kernel(T* trunk, const T* src, int len, int max_trunk, int row_elems, const int32_t* pages, int page_stride,
+                                  int64_t total) {
   int64_t idx = (int64_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (idx >= total) return;
   int64_t per_seq = (int64_t)len * row_elems;
   int64_t b = idx / per_seq, rem = idx % per_seq;
-  trunk[b * (int64_t)max_trunk * row_elems + rem] = src[idx];
+  if (pages) {
+    const int64_t pos = rem / row_elems, page = pages[b * page_stride + (pos >> 5)];
+    trunk[(page * 32 + (pos & 31)) * row_elems + rem % row_elems] = src[idx];
+  } else {
+    trunk[b * (int64_t)max_trunk * row_elems + rem] = src[idx];
+  }
 }
 
 inline int grid_for(int64_t n) { return (int)((n + kBlock - 1) / kBlock); }
@@ -287,12 +294,12 @@ inline int grid_for(int64_t n) { return (int)((n + kBlock - 1) / kBlock); }
 static int embed_blocks(const EmbedGather& e, int M) { return e.table ? M * ((e.d / 4 + kBlock - 1) / kBlock) : 0; }
 
 int launch_setup_branch_rows(RowDesc* rows, float* cos_sin, const int32_t* trunk_len, int B, int K, const FanTable& fan, int step,
-                             int half_dim, float theta, int32_t* step_tokens, const int32_t* keys,
+                             int half_dim, float theta, const RopeScaling& scaling, int32_t* step_tokens, const int32_t* keys,
                              const int32_t* cache_tokens, const int32_t* forced_keys, const int32_t* forced_tokens,
                              const EmbedGather& embed, hipStream_t s) {
   const int M = B * fan.off[K + 1];
   const int blocks = grid_for((int64_t)M * half_dim);
-  setup_branch_rows_kernel<<<blocks + embed_blocks(embed, M), kBlock, 0, s>>>(rows, cos_sin, trunk_len, M, K, fan, step, half_dim, theta,
+  setup_branch_rows_kernel<<<blocks + embed_blocks(embed, M), kBlock, 0, s>>>(rows, cos_sin, trunk_len, M, K, fan, step, half_dim, theta, scaling,
                                                                               step_tokens, keys, cache_tokens, forced_keys, forced_tokens,
                                                                               embed, blocks);
   SSD_HIP(hipGetLastError());
@@ -300,10 +307,11 @@ int launch_setup_branch_rows(RowDesc* rows, float* cos_sin, const int32_t* trunk
 }
 
 int launch_setup_extend_rows(RowDesc* rows, float* cos_sin, const int32_t* trunk_len, const int32_t* limit, int B, int T, int offset,
-                             int half_dim, float theta, int seq_base, const EmbedGather& embed, const int32_t* tokens, hipStream_t s) {
+                             int half_dim, float theta, const RopeScaling& scaling, int seq_base, const EmbedGather& embed,
+                             const int32_t* tokens, hipStream_t s) {
   const int blocks = grid_for((int64_t)B * T * half_dim);
   setup_extend_rows_kernel<<<blocks + embed_blocks(embed, B * T), kBlock, 0, s>>>(rows, cos_sin, trunk_len, limit, B, T, offset, half_dim,
-                                                                                  theta, seq_base, embed, tokens, blocks);
+                                                                                  theta, scaling, seq_base, embed, tokens, blocks);
   SSD_HIP(hipGetLastError());
   return SSD_OK;
 }
@@ -358,16 +366,16 @@ int launch_pending_exclude(int32_t* exclude, const int32_t* pending, int B, int 
   return SSD_OK;
 }
 
-int launch_copy_kv_in(int dtype, void* trunk, const void* src, int B, int len, int max_trunk, int row_elems,
-                      hipStream_t s) {
+int launch_copy_kv_in(int dtype, void* trunk, const void* src, int B, int len, int max_trunk, int row_elems, const int32_t* pages,
+                      int page_stride, hipStream_t s) {
   int64_t total = (int64_t)B * len * row_elems;
   if (total == 0) return SSD_OK;
   if (dtype == SSD_BF16)
     copy_kv_in_kernel<bf16_t><<<grid_for(total), kBlock, 0, s>>>((bf16_t*)trunk, (const bf16_t*)src, len, max_trunk,
-                                                                row_elems, total);
+                                                                row_elems, pages, page_stride, total);
   else
     copy_kv_in_kernel<float><<<grid_for(total), kBlock, 0, s>>>((float*)trunk, (const float*)src, len, max_trunk,
-                                                               row_elems, total);
+                                                               row_elems, pages, page_stride, total);
   SSD_HIP(hipGetLastError());
   return SSD_OK;
 }

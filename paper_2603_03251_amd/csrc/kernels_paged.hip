@@ -691,6 +691,15 @@ size_t paged_attention_workspace(int B, int T, int n_q, int n_kv, int head_dim, 
   return (size_t)B * T * n_q * n * (head_dim + 2) * sizeof(float);
 }
 
+// (splits grow with the positions until there are 256 blocks)
+size_t paged_attention_workspace_bound(int B, int T, int n_q, int n_kv, int head_dim, int max_visible) {
+  const int tiles = (int)(((int64_t)T * (n_q / n_kv) + 15) / 16);
+  const int64_t units = (int64_t)B * n_kv * ((tiles + 1) / 2), steps = max_visible / kSplitStep + 1;
+  int64_t n = units < 256 ? 256 / units : 1;
+  n = n < steps ? n : steps;
+  return (size_t)B * T * n_q * n * (head_dim + 2) * sizeof(float);
+}
+
 int launch_paged_attention(int dtype, int cache_dtype, const PagedAttnArgs& a, hipStream_t s) {
   if (dtype == SSD_BF16) return cache_dtype == SSD_BF16 ? launch_types<bf16_t, bf16_t>(a, s) : launch_types<bf16_t, float>(a, s);
   return cache_dtype == SSD_BF16 ? launch_types<float, bf16_t>(a, s) : launch_types<float, float>(a, s);

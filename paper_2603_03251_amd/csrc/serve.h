@@ -31,6 +31,9 @@ struct RopeArgs {
   int n_pages, page_size, table_stride;
   int head_groups;   // set by the launcher
 };
+// The settings as the kernels take them; EINVAL (and a message that starts with `who`) where they make no rotation.
+int rope_scaling(const char* who, const ssd_rope_config* r, int head_dim, RopeScaling* out);
+void rope_turns(float theta, int rot, const RopeScaling& scaling, RopeTurns* out);
 int launch_rope(int dtype, int cache_dtype, const RopeArgs& a, const RopeTurns& f, hipStream_t s);
 
 // Rows b T .. b T + T - 1 are sequence b's; row r sees positions 0 .. visible[r vis_step] - 1 of its pages, at most max_visible, and
@@ -55,6 +58,8 @@ struct PagedAttnArgs {
 };
 int launch_paged_attention(int dtype, int cache_dtype, const PagedAttnArgs& a, hipStream_t s);
 size_t paged_attention_workspace(int B, int T, int n_q, int n_kv, int head_dim, int max_visible);
+// enough for any max_visible up to this one, which may change from call to call
+size_t paged_attention_workspace_bound(int B, int T, int n_q, int n_kv, int head_dim, int max_visible);
 
 struct VerifyProbsArgs {
   const float *target, *draft;   // [B][K + 1][V] and [B][K][V], rows target_ld and draft_ld apart; draft null: the tokens were certain

@@ -5,11 +5,11 @@
 
 using namespace ssd;
 
-namespace {
+namespace ssd {
 
 constexpr double kTwoPi = 6.283185307179586476925;
 
-int check_rope(const char* who, const ssd_rope_config* r, int32_t head_dim) {
+int rope_scaling(const char* who, const ssd_rope_config* r, int head_dim, RopeScaling* out) {
   SSD_CHECK_ARG(head_dim == 64 || head_dim == 128, "%s: head_dim %d not supported (64 or 128)", who, head_dim);
   SSD_CHECK_ARG(r->rot_dim >= 2 && r->rot_dim <= head_dim && r->rot_dim % 2 == 0, "%s: rot_dim %d must be even, in 2..head_dim", who, r->rot_dim);
   SSD_CHECK_ARG(r->layout == SSD_ROPE_HALF || r->layout == SSD_ROPE_INTERLEAVED, "%s: layout %d unknown", who, r->layout);
@@ -20,33 +20,27 @@ int check_rope(const char* who, const ssd_rope_config* r, int32_t head_dim) {
   if (r->scaling >= SSD_ROPE_BANDS)
     SSD_CHECK_ARG(r->original > 0.f && isfinite(r->original) && r->low > 0.f && r->high > r->low && isfinite(r->high),
                   "%s: original > 0 and 0 < low < high required", who);
+  *out = {r->scaling, r->factor, r->low, r->high, r->original, r->magnitude, 0.f, 0.f};
+  if (r->scaling == SSD_ROPE_RAMP) {
+    const double per_log = r->rot_dim / (2.0 * log((double)r->theta));
+    out->i0 = (float)fmax(floor(per_log * log((double)r->original / (kTwoPi * r->high))), 0.0);
+    out->i1 = (float)fmin(ceil(per_log * log((double)r->original / (kTwoPi * r->low))), r->rot_dim - 1.0);
+  }
   return SSD_OK;
 }
 
 // Turns per position of every pair, in fp64.
-void rope_turns(const ssd_rope_config* r, RopeTurns* out) {
-  const int half = r->rot_dim / 2;
-  const double log2_theta = log2((double)r->theta);
-  double i0 = 0.0, i1 = 0.0;
-  if (r->scaling == SSD_ROPE_RAMP) {
-    const double per_log = r->rot_dim / (2.0 * log2_theta);
-    i0 = fmax(floor(per_log * log2((double)r->original / (kTwoPi * r->high))), 0.0);
-    i1 = fmin(ceil(per_log * log2((double)r->original / (kTwoPi * r->low))), r->rot_dim - 1.0);
-  }
+void rope_turns(float theta, int rot, const RopeScaling& scaling, RopeTurns* out) {
+  const double log2_theta = log2((double)theta);
   for (int i = 0; i < kMaxPairs; ++i) {
-    double t = i < half ? exp2(-2.0 * i / r->rot_dim * log2_theta) / kTwoPi : 0.0;
-    if (r->scaling == SSD_ROPE_LINEAR) t /= r->factor;
-    if (r->scaling == SSD_ROPE_BANDS) {
-      const double keep = fmin(fmax((r->original * t - r->low) / ((double)r->high - r->low), 0.0), 1.0);
-      t *= keep + (1.0 - keep) / r->factor;
-    }
-    if (r->scaling == SSD_ROPE_RAMP) {
-      const double slow = fmin(fmax((i - i0) / fmax(i1 - i0, 1e-3), 0.0), 1.0);
-      t *= 1.0 - slow + slow / r->factor;
-    }
-    out->turns[i] = t;
+    const double t = i < rot / 2 ? exp2(-2.0 * i / rot * log2_theta) / kTwoPi : 0.0;
+    out->turns[i] = t * rope_share(scaling, t, i);
   }
 }
+
+}  // namespace ssd
+
+namespace {
 
 int check_paged_kv(const char* who, const ssd_paged_kv* kv) {
   SSD_CHECK_ARG(kv->d_k && kv->d_v && kv->d_table, "%s: null pointer in the cache", who);
@@ -74,13 +68,14 @@ extern "C" {
 int ssd_rope(const ssd_rope_config* rope, const void* d_x, int64_t x_ld, int32_t dtype, const int32_t* d_positions, int32_t rows,
              int32_t n_heads, int32_t head_dim, void* d_out, int64_t out_ld, void* stream) {
   SSD_CHECK_ARG(rope && (rows == 0 || (d_x && d_positions && d_out)), "ssd_rope: null argument");
-  SSD_TRY(check_rope("ssd_rope", rope, head_dim));
+  RopeScaling scaling;
+  SSD_TRY(rope_scaling("ssd_rope", rope, head_dim, &scaling));
   SSD_CHECK_ARG(dtype_ok(dtype), "ssd_rope: dtype %d unknown", dtype);
   SSD_CHECK_ARG(rows >= 0 && rows <= (1 << 24) && n_heads >= 1 && n_heads <= 1024 && (int64_t)rows * n_heads <= (1 << 28),
                 "ssd_rope: rows in 0..2^24, n_heads in 1..1024 and at most 2^28 of both together required");
   SSD_CHECK_ARG(x_ld >= (int64_t)n_heads * head_dim && out_ld >= (int64_t)n_heads * head_dim, "ssd_rope: a row must hold its heads");
   RopeTurns turns;
-  rope_turns(rope, &turns);
+  rope_turns(rope->theta, rope->rot_dim, scaling, &turns);
   RopeArgs a = {};
   a.q = d_x; a.q_ld = x_ld; a.q_out = d_out; a.q_out_ld = out_ld;
   a.positions = d_positions; a.row_step = 1; a.rows = rows; a.rows_per_seq = 1;
@@ -94,7 +89,8 @@ int ssd_rope_append(const ssd_rope_config* rope, const ssd_paged_kv* kv, const v
                     int32_t n_q_heads, void* d_q_out, int64_t q_out_ld, void* stream) {
   SSD_CHECK_ARG(rope && kv && (B == 0 || (d_q && d_k && d_v && d_positions && d_q_out)), "ssd_rope_append: null argument");
   SSD_TRY(check_paged_kv("ssd_rope_append", kv));
-  SSD_TRY(check_rope("ssd_rope_append", rope, kv->head_dim));
+  RopeScaling scaling;
+  SSD_TRY(rope_scaling("ssd_rope_append", rope, kv->head_dim, &scaling));
   SSD_CHECK_ARG(dtype_ok(dtype), "ssd_rope_append: dtype %d unknown", dtype);
   SSD_CHECK_ARG(B >= 0 && T >= 1 && (int64_t)B * T <= (1 << 24), "ssd_rope_append: B >= 0, T >= 1 and at most 2^24 rows required");
   SSD_CHECK_ARG(n_q_heads >= 1 && n_q_heads <= 1024 && (int64_t)B * T * (n_q_heads + 2 * kv->n_kv_heads) <= (1 << 28),
@@ -102,7 +98,7 @@ int ssd_rope_append(const ssd_rope_config* rope, const ssd_paged_kv* kv, const v
   const int64_t qd = (int64_t)n_q_heads * kv->head_dim, kvd = (int64_t)kv->n_kv_heads * kv->head_dim;
   SSD_CHECK_ARG(q_ld >= qd && q_out_ld >= qd && k_ld >= kvd && v_ld >= kvd, "ssd_rope_append: a row must hold its heads");
   RopeTurns turns;
-  rope_turns(rope, &turns);
+  rope_turns(rope->theta, rope->rot_dim, scaling, &turns);
   RopeArgs a = {};
   a.q = d_q; a.q_ld = q_ld; a.k = d_k; a.k_ld = k_ld; a.v = d_v; a.v_ld = v_ld; a.q_out = d_q_out; a.q_out_ld = q_out_ld;
   a.positions = d_positions; a.slots = d_slots ? d_slots : d_positions; a.row_step = 1; a.rows = B * T; a.rows_per_seq = T;

@@ -18,6 +18,7 @@
 #include "common.h"
 #include "f32_head.h"
 #include "fused.h"
+#include "serve.h"
 #include "wide_blocks.h"
 
 namespace ssd {
@@ -79,6 +80,7 @@ using namespace ssd;
 
 struct ssd_model {
   Dims dims;
+  RopeScaling rope = {SSD_ROPE_PLAIN, 1.f, 0.f, 0.f, 0.f, 1.f, 0.f, 0.f};   // theta is in dims
   int tie;
   Arena arena;
   void* embed = nullptr;       // row-major [V][d]
@@ -550,6 +552,37 @@ EmbedGather embed_gather(const ssd_ctx* c) {
 // One batched pass of the decoder over `M` rows whose descriptors and rotary tables are already in ctx->rows /
 // ctx->cos_sin (and, where embed_gather says so, whose embeddings are in ctx->h).  Logits (fp32, row stride logits_ld) and final-norm
 // hidden states are optional.
+// Rotary positions, append and attention of layer l in a context of per-operator kernels with a paged trunk: the serving operators on the
+// pass's own buffers.  An extend's keys go to the trunk's pages; a branch row's to its private suffix, a page of K positions of its own, which
+// its attention sees behind the trunk.
+int paged_attention_of(ssd_ctx* c, int l, const RopeTurns& turns, int nb, int rows_per_seq, int max_vis, int branch_depth, int seq_base, hipStream_t s) {
+  const Dims& d = c->model->dims;
+  const bool branch = branch_depth >= 0;
+  constexpr int kRow = sizeof(RowDesc) / sizeof(int32_t);
+  const int32_t* table = c->page_table_dev + (size_t)seq_base * c->page_stride;
+  RopeArgs r = {};
+  r.q = c->qkv; r.k = c->qkv + d.q_dim(); r.v = c->qkv + d.q_dim() + d.kv_dim();
+  r.q_ld = r.k_ld = r.v_ld = d.qkv_dim();
+  r.q_out = c->q; r.q_out_ld = d.q_dim();
+  r.positions = &c->rows->pos; r.slots = &c->rows->kv_slot; r.row_step = kRow; r.rows = nb * rows_per_seq; r.rows_per_seq = rows_per_seq;
+  r.n_q = d.n_q_heads; r.n_kv = d.n_kv_heads; r.head_dim = r.rot = d.head_dim; r.magnitude = c->model->rope.magnitude;
+  r.pool_k = branch ? c->suffix_k[l] : c->trunk_k[l]; r.pool_v = branch ? c->suffix_v[l] : c->trunk_v[l];
+  r.table = branch ? nullptr : table; r.page_size = branch ? c->K : 32; r.page_stride = (int64_t)r.page_size * d.kv_dim();
+  r.n_pages = branch ? r.rows : c->kv_pages; r.table_stride = branch ? 1 : c->page_stride;
+  SSD_TRY(launch_rope(SSD_F32, d.dtype, r, turns, s));
+  PagedAttnArgs a = {};
+  a.q = c->q; a.q_ld = a.out_ld = d.q_dim();
+  a.k = c->trunk_k[l]; a.v = c->trunk_v[l]; a.table = table; a.page_stride = (int64_t)32 * d.kv_dim();
+  a.n_pages = c->kv_pages; a.page_shift = 5; a.table_stride = c->page_stride;
+  a.visible = &c->rows->vis; a.vis_step = kRow; a.B = nb; a.T = rows_per_seq; a.n_q = d.n_q_heads; a.n_kv = d.n_kv_heads; a.head_dim = d.head_dim;
+  // (the tokens of an extend are trunk positions too: they are appended before the attention runs)
+  a.max_visible = std::min(max_vis + (branch ? 0 : rows_per_seq), c->max_trunk);
+  a.scale_log2 = 1.44269504088896341f / sqrtf((float)d.head_dim);
+  if (branch) { a.tail_k = c->suffix_k[l]; a.tail_v = c->suffix_v[l]; a.tail_cap = c->K; a.tail_len = branch_depth + 1; }
+  a.out = c->attn_out; a.out_plane = d.dtype == SSD_BF16 ? (int64_t)c->max_rows * d.q_dim() : 0; a.workspace = c->attn_partial;
+  return launch_paged_attention(SSD_F32, d.dtype, a, s);
+}
+
 // max_vis: host bound of the stored trunk positions any row sees; branch_depth: decode step of branch rows, -1 for an extend.
 // wide: fused contexts run the pass as wide passes.
 int forward_rows(ssd_ctx* c, bool wide, int M, const int32_t* tokens, int rows_per_seq, int max_vis, int branch_depth, float* logits,
@@ -560,9 +593,15 @@ int forward_rows(ssd_ctx* c, bool wide, int M, const int32_t* tokens, int rows_p
     return fused_forward(c, wide, M, tokens, rows_per_seq, max_vis, branch_depth, logits, logits_ld, hidden, hidden_ld, seq_base, s);
   const int dt = d.dtype;
   const int64_t R = c->max_rows;     // plane stride of an activation buffer = R * columns
+  RopeTurns turns;
+  if (c->kv_pages) rope_turns(d.rope_theta, d.head_dim, m->rope, &turns);
   for (int l = 0; l < d.n_layers; ++l) {
     const ssd_model::Layer& L = m->layers[l];
-    if (dt == SSD_F32) {
+    if (c->kv_pages) {
+      SSD_TRY(launch_rmsnorm(dt, c->h, L.attn_norm, c->xn, R * d.d_model, nullptr, 0, M, d.d_model, d.rms_eps, s));
+      SSD_TRY(launch_gemm(dt, EPI_STORE_F32, c->xn, R * d.d_model, L.wqkv, nullptr, c->qkv, d.qkv_dim(), 0, M, d.qkv_dim(), d.d_model, s));
+      SSD_TRY(paged_attention_of(c, l, turns, M / rows_per_seq, rows_per_seq, max_vis, branch_depth, seq_base, s));
+    } else if (dt == SSD_F32) {
       SSD_TRY(launch_norm_qkv_rope_f32(c->h, (const float*)L.attn_norm, (const float*)L.wqkv, c->q, (float*)c->trunk_k[l],
                                        (float*)c->trunk_v[l], (float*)c->suffix_k[l], (float*)c->suffix_v[l], c->rows, c->cos_sin,
                                        M, d, c->max_trunk, c->K, s));
@@ -573,14 +612,16 @@ int forward_rows(ssd_ctx* c, bool wide, int M, const int32_t* tokens, int rows_p
       SSD_TRY(launch_rope_append(c->qkv, c->rows, c->cos_sin, c->q, c->trunk_k[l], c->trunk_v[l], c->suffix_k[l],
                                  c->suffix_v[l], M, d.n_q_heads, d.n_kv_heads, d.head_dim, c->max_trunk, c->K, s));
     }
-    AttnArgs a;
-    a.q = c->q; a.trunk_k = c->trunk_k[l]; a.trunk_v = c->trunk_v[l]; a.suffix_k = c->suffix_k[l];
-    a.suffix_v = c->suffix_v[l]; a.out = c->attn_out; a.out_plane = R * d.q_dim(); a.rows = c->rows; a.partial = c->attn_partial; a.partial_floats = c->attn_partial_floats; a.M = M;
-    a.n_q_heads = d.n_q_heads; a.n_kv_heads = d.n_kv_heads; a.head_dim = d.head_dim; a.max_trunk = c->max_trunk;
-    a.suffix_cap = c->K; a.rows_per_seq = rows_per_seq; a.extend = branch_depth < 0;
-    // here the tokens of an extend are trunk positions too (they are appended before the attention runs)
-    a.max_vis = max_vis + (branch_depth < 0 ? rows_per_seq : 0);
-    SSD_TRY(launch_attention(dt, a, s));
+    if (!c->kv_pages) {
+      AttnArgs a;
+      a.q = c->q; a.trunk_k = c->trunk_k[l]; a.trunk_v = c->trunk_v[l]; a.suffix_k = c->suffix_k[l];
+      a.suffix_v = c->suffix_v[l]; a.out = c->attn_out; a.out_plane = R * d.q_dim(); a.rows = c->rows; a.partial = c->attn_partial; a.partial_floats = c->attn_partial_floats; a.M = M;
+      a.n_q_heads = d.n_q_heads; a.n_kv_heads = d.n_kv_heads; a.head_dim = d.head_dim; a.max_trunk = c->max_trunk;
+      a.suffix_cap = c->K; a.rows_per_seq = rows_per_seq; a.extend = branch_depth < 0;
+      // here the tokens of an extend are trunk positions too (they are appended before the attention runs)
+      a.max_vis = max_vis + (branch_depth < 0 ? rows_per_seq : 0);
+      SSD_TRY(launch_attention(dt, a, s));
+    }
     SSD_TRY(launch_gemm(dt, EPI_RESIDUAL_ADD, c->attn_out, R * d.q_dim(), L.wo, nullptr, c->h, d.d_model, 0, M, d.d_model,
                         d.q_dim(), s));
     if (dt == SSD_F32) {
@@ -633,7 +674,7 @@ int extend_rows(ssd_ctx* c, bool wide, const int32_t* tokens, int T, int offset,
   const Dims& d = c->model->dims;
   SSD_TRY(pages_for_pass(c, b0, nb, offset + T, h_limit, s));
   SSD_TRY(launch_setup_extend_rows(c->rows, c->cos_sin, c->trunk_len, h_limit ? c->prompt_len : nullptr, nb, T, offset, d.head_dim / 2,
-                                   d.rope_theta, b0, embed_gather(c), tokens, s));
+                                   d.rope_theta, c->model->rope, b0, embed_gather(c), tokens, s));
   int ub = 0;
   for (int b = b0; b < b0 + nb; ++b) ub = c->ub_of[b] > ub ? c->ub_of[b] : ub;
   if (wide && takes_small_pass(c, nb, T, ub + offset, s)) wide = false;
@@ -912,6 +953,17 @@ int ssd_model_create(const ssd_model_config* cfg, const ssd_model_weights* w, vo
   return SSD_OK;
 }
 
+int ssd_model_set_rope(ssd_model* m, const ssd_rope_config* rope) {
+  SSD_CHECK_ARG(m && rope, "ssd_model_set_rope: null argument");
+  RopeScaling scaling;
+  SSD_TRY(rope_scaling("ssd_model_set_rope", rope, m->dims.head_dim, &scaling));
+  SSD_CHECK_ARG(rope->layout == SSD_ROPE_HALF && rope->rot_dim == m->dims.head_dim,
+                "ssd_model_set_rope: a model's heads are rotated as a whole, in pairs (i, i + head_dim / 2)");
+  m->dims.rope_theta = rope->theta;
+  m->rope = scaling;
+  return SSD_OK;
+}
+
 int ssd_model_release_operator_weights(ssd_model* m) {
   SSD_CHECK_ARG(m, "ssd_model_release_operator_weights: null model");
   if (!m->operator_weights) return SSD_OK;
@@ -1025,13 +1077,18 @@ static int ctx_create(const ssd_model* model, const ssd_round_config* cfg, const
   c->blocks_of.assign(c->B, 0);
   if (cfg->kv_pages) {
     // paged trunk (App. B): a pool of 32-position pages per layer instead of max_trunk positions per sequence
-    if (!c->fused_mode || d.head_dim != 64) {
-      set_error("kv_pages: the paged trunk is served by the fused passes only (bf16 model of a supported shape, no SSD_CTX_PER_OPERATOR)");
+    if (cfg->flags & SSD_CTX_PER_OPERATOR) {
+      set_error("kv_pages: SSD_CTX_PER_OPERATOR asks for the kernels of the contiguous trunk");
       ssd_ctx_destroy(c);
       return SSD_EINVAL;
     }
-    if (cfg->kv_pages < 2 || c->max_trunk > 16384) {
-      set_error("kv_pages must be at least 2 (page 0 is the shared all-zero page) and max_trunk at most 16384 in a paged context");
+    if (cfg->kv_pages < 2 || (c->fused_mode && c->max_trunk > 16384)) {
+      set_error("kv_pages must be at least 2 (page 0 is the shared all-zero page) and max_trunk at most 16384 in a paged context of fused passes");
+      ssd_ctx_destroy(c);
+      return SSD_EINVAL;
+    }
+    if (!c->fused_mode && (c->B > 65535 || (int64_t)c->max_rows * d.n_q_heads > (1 << 23))) {
+      set_error("kv_pages: at most 65535 sequences and 2^23 rows x query heads in a paged context of per-operator kernels");
       ssd_ctx_destroy(c);
       return SSD_EINVAL;
     }
@@ -1079,6 +1136,14 @@ static int ctx_create(const ssd_model* model, const ssd_round_config* cfg, const
     A(&c->attn_out, sizeof(float) * (size_t)R * d.q_dim());
     A(&c->act, sizeof(float) * (size_t)R * d.d_ffn);
     c->attn_partial_floats = attention_partial_floats(R, d.n_q_heads, d.head_dim, c->max_trunk + c->K);
+    if (c->kv_pages) {
+      // passes of one sequence or of all, of any number of tokens an extend takes, or of the branch rows
+      size_t most = 0;
+      for (int nb : {1, c->B})
+        for (int t = 1; t <= c->K + 2; ++t)
+          most = std::max(most, paged_attention_workspace_bound(nb, t <= c->K + 1 ? t : c->rows_per_seq, d.n_q_heads, d.n_kv_heads, d.head_dim, c->max_trunk));
+      c->attn_partial_floats = (int64_t)(most / sizeof(float));
+    }
     A((void**)&c->attn_partial, (size_t)c->attn_partial_floats * sizeof(float));
   }
   A(&c->sample_scratch, sample_scratch_bytes(c->M));
@@ -1292,8 +1357,11 @@ int ssd_ctx_load_trunk(ssd_ctx* c, const void* d_k, const void* d_v, int32_t len
                                    (const bf16_t*)((const char*)d_v + l * per_layer), c->B, len, d.n_kv_heads, c->vt_stride,
                                    c->kv_pages ? c->page_table_dev : nullptr, c->page_stride, s));
     } else {
-      SSD_TRY(launch_copy_kv_in(d.dtype, c->trunk_k[l], (const char*)d_k + l * per_layer, c->B, len, c->max_trunk, d.kv_dim(), s));
-      SSD_TRY(launch_copy_kv_in(d.dtype, c->trunk_v[l], (const char*)d_v + l * per_layer, c->B, len, c->max_trunk, d.kv_dim(), s));
+      const int32_t* pages = c->kv_pages ? c->page_table_dev : nullptr;
+      SSD_TRY(launch_copy_kv_in(d.dtype, c->trunk_k[l], (const char*)d_k + l * per_layer, c->B, len, c->max_trunk, d.kv_dim(), pages,
+                                c->page_stride, s));
+      SSD_TRY(launch_copy_kv_in(d.dtype, c->trunk_v[l], (const char*)d_v + l * per_layer, c->B, len, c->max_trunk, d.kv_dim(), pages,
+                                c->page_stride, s));
     }
   }
   SSD_TRY(launch_fill_i32(c->trunk_len, len, c->B, s));
@@ -1402,7 +1470,7 @@ int ssd_prespeculate(ssd_ctx* c, const int32_t* d_pending, const float* d_temper
   SSD_TRY(mark());
   // a2/a3: K batched branch-decode steps; logits and tokens land in the cache directly
   for (int i = 0; i < K; ++i) {
-    SSD_TRY(launch_setup_branch_rows(c->rows, c->cos_sin, c->trunk_len, B, K, c->fan, i, d.head_dim / 2, d.rope_theta, c->step_tokens,
+    SSD_TRY(launch_setup_branch_rows(c->rows, c->cos_sin, c->trunk_len, B, K, c->fan, i, d.head_dim / 2, d.rope_theta, c->model->rope, c->step_tokens,
                                      c->keys, c->tokens, c->forced_keys, c->forced_tokens, embed_gather(c), s));
     SSD_TRY(forward_rows(c, c->fused_wide, M, c->step_tokens, RB, c->trunk_ub + K + 1, i, c->logits + (size_t)i * V, (int64_t)K * V,
                          c->hidden + (size_t)i * d.d_model, (int64_t)K * d.d_model, 0, s));
