@@ -379,7 +379,8 @@ typedef struct ssd_rope_config {
 
 /* One layer's keys and values in pages.  Position t of sequence b is position t % page_size of page d_table[b][t / page_size]; KV head h
  * and dimension d of it are element (page page_stride) + ((t % page_size) n_kv_heads + h) head_dim + d of d_k and d_v.  An entry outside
- * 0 .. n_pages - 1 names no page: nothing is stored there, and attention does not see its positions. */
+ * 0 .. n_pages - 1 names no page: nothing is stored there, and attention does not see its positions.
+ * Several sequences may name the same page (a shared prefix), of which a call then must not store any. */
 typedef struct {
   void *d_k, *d_v;          /* 16-byte aligned */
   const int32_t* d_table;   /* [B][table_stride] */
@@ -393,7 +394,7 @@ typedef struct {
 } ssd_paged_kv;
 
 /* Keys and values that one row alone sees, behind its positions in the pages (a branch's own tokens): [B][T][capacity][n_kv_heads][head_dim]
- * of the cache's dtype, 16-byte aligned, of which every row sees the first `length`. */
+ * of the cache's dtype, of which every row sees the first `length`. */
 typedef struct {
   const void *d_k, *d_v;
   int32_t capacity;         /* 1..256 */
@@ -417,7 +418,7 @@ int ssd_rope_append(const ssd_rope_config* rope, const ssd_paged_kv* kv, const v
  * 0 .. d_visible[b][t] - 1 of sequence b's pages (negative: none; values above max_visible count as max_visible) and the row's tail
  * (tail NULL: none).  A block of T tokens appended at positions n .. n + T - 1 has visible = n + 1 + t.  A row that sees nothing gives zeros.
  * What a row does not see does not reach it, whatever is stored there (infinities, NaN).
- *   dtype        of queries and output; their bases and rows, and the workspace, start on 16 bytes.
+ *   dtype        of queries and output; their bases and rows, and the workspace, start on 16 bytes.  d_out with out_ld may be d_q with q_ld.
  *   max_visible  host bound of d_visible: sizes the launch, at most table_stride page_size.
  *   d_lse        float [B][T][n_q_heads] or NULL: ln sum_j exp(scale q k_j), -inf for a row that sees nothing (joins of parts computed elsewhere).
  *   d_workspace  ssd_paged_attention_workspace_bytes() of device memory for these sizes, private to the call until `stream` has passed it. */
@@ -436,8 +437,8 @@ size_t ssd_paged_attention_workspace_bytes(const ssd_paged_kv* kv, int32_t B, in
  * s_{i+1} is accepted while u_i q(s) < p(s), in exact arithmetic; a token outside 0..V-1 is not.  bonus = the first token whose cumulative
  * mass exceeds u_bonus times the whole, the mass max(p - q, 0) at the first rejected row (p itself where nothing is left of it) and p
  * behind the last accepted token, summed in fp64; values outside [0,1) are kept within.  A row without mass gives bonus -1.
- *   out: d_accept_len int32 [B], d_bonus int32 [B].  d_workspace: ssd_verify_probs_workspace_bytes(B, V), 16-byte aligned, private to the
- *   call until `stream` has passed it.  EINVAL for K outside 1..SSD_MAX_K, V < 2, null pointers. */
+ *   out: d_accept_len int32 [B], d_bonus int32 [B], which must not overlap each other or an input.  d_workspace:
+ *   ssd_verify_probs_workspace_bytes(B, V), 16-byte aligned, private to the call until `stream` has passed it.  EINVAL for K outside 1..SSD_MAX_K, V < 2, null pointers. */
 int ssd_verify_probs(const float* d_target_probs, int64_t target_ld, const float* d_draft_probs, int64_t draft_ld, const int32_t* d_spec_tokens,
                      const int32_t* d_drafted, const float* d_u_accept, const float* d_u_bonus, int32_t B, int32_t K, int32_t V,
                      int32_t* d_accept_len, int32_t* d_bonus, void* d_workspace, void* stream);

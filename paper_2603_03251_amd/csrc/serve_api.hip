@@ -124,8 +124,9 @@ int ssd_paged_attention(const ssd_paged_kv* kv, const void* d_q, int64_t q_ld, i
   SSD_CHECK_ARG(dtype_ok(dtype), "ssd_paged_attention: dtype %d unknown", dtype);
   SSD_CHECK_ARG(n_q_heads >= 1 && n_q_heads <= 1024 && n_q_heads % kv->n_kv_heads == 0,
                 "ssd_paged_attention: n_q_heads must be a multiple of n_kv_heads, at most 1024");
-  SSD_CHECK_ARG(B >= 0 && B <= 65535 && T >= 1 && T <= 65535 && (int64_t)B * T * n_q_heads <= (1 << 23),
-                "ssd_paged_attention: B in 0..65535, T in 1..65535 and at most 2^23 rows x heads required");
+  SSD_CHECK_ARG(B >= 0 && B <= 65535 && T >= 1 && T <= 65535 && (int64_t)B * T * n_q_heads <= (1 << 23) &&
+                    (int64_t)T * (n_q_heads / kv->n_kv_heads) <= 16 * 65535,
+                "ssd_paged_attention: B in 0..65535, T in 1..65535, at most 2^23 rows x heads and 16 x 65535 rows x heads of a KV head and sequence required");
   SSD_CHECK_ARG(max_visible >= 0 && max_visible <= (1 << 30) && max_visible <= (int64_t)kv->table_stride * kv->page_size,
                 "ssd_paged_attention: max_visible %d exceeds the block table", max_visible);
   SSD_CHECK_ARG(isfinite(scale), "ssd_paged_attention: scale must be finite");

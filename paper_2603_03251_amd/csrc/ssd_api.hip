@@ -1087,7 +1087,9 @@ static int ctx_create(const ssd_model* model, const ssd_round_config* cfg, const
       ssd_ctx_destroy(c);
       return SSD_EINVAL;
     }
-    if (!c->fused_mode && (c->B > 65535 || (int64_t)c->max_rows * d.n_q_heads > (1 << 23))) {
+    if (!c->fused_mode && (c->B > 65535 || (int64_t)c->max_rows * d.n_q_heads > (1 << 23) ||
+                           (int64_t)std::max(c->rows_per_seq, c->K + 1) * (d.n_q_heads / d.n_kv_heads) > 16 * 65535 ||
+                           (int64_t)32 * d.kv_dim() > (1 << 29))) {
       set_error("kv_pages: at most 65535 sequences and 2^23 rows x query heads in a paged context of per-operator kernels");
       ssd_ctx_destroy(c);
       return SSD_EINVAL;

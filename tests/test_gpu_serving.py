@@ -317,6 +317,43 @@ def test_blocks_of_two_tiles(B, D):
     check_attention(B, c, q, np.minimum(visible, n - 6), tail=(tk, tv, 2), max_visible=n)
 
 
+@pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("nb,T,hq,hkv,D,page,n", [(1, 1, 64, 1, 128, 1024, 1500), (1, 70, 48, 1, 64, 32, 90), (130, 1, 2, 2, 64, 64, 70),
+                                                  (2, 3, 5, 5, 128, 256, 400)])
+def test_other_shapes(B, dtype, cache, nb, T, hq, hkv, D, page, n):
+    """Many heads of one KV head, many rows, many sequences, pages larger than a step of all wavefronts."""
+    g = gen(nb + T)
+    c = _full_cache(B, g, nb, n, page, hkv, D, cache)
+    check_attention(B, c, randn(g, (nb, T, hq, D), dtype), np.random.default_rng(nb).integers(0, n + 1, (nb, T)), max_visible=n)
+
+
+def test_calls_on_two_streams_and_shared_pages(B):
+    """Calls that overlap on two streams with a workspace each give the bits of calls one after the other; two sequences with the same pages; in
+    place."""
+    g = gen(31)
+    c = _full_cache(B, g, 2, 2000, 32, 4, 128, BF16)
+    table = c.table.copy()
+    table[1, :40] = table[0, :40]
+    c.set_table(table)
+    qs = [randn(g, (2, 5, 16, 128), BF16) for _ in range(2)]
+    vis = np.array([[1996, 1997, 1998, 1999, 2000], [1280, 1281, 1400, 700, 1]])
+    want = [check_attention(B, c, q, vis)[0] for q in qs]
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.empty_like(q) for q in qs]
+    n = B.ssd_paged_attention_workspace_bytes(c.kv, 2, 5, 16, 2000)
+    ws, v = [torch.empty(n, dtype=torch.uint8, device="cuda") for _ in range(2)], i32(vis)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, q, o, w in zip(streams, qs, outs, ws):
+            B.ssd_paged_attention(c.kv, q, v, 2000, o, w, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
+    for most in (2000, 200):                             # split and joined, and in one launch
+        q, o = qs[0].clone(), torch.empty_like(qs[0])
+        B.ssd_paged_attention(c.kv, q, v, most, o, ws[0])
+        B.ssd_paged_attention(c.kv, q, v, most, q, ws[0])
+        assert torch.equal(q, o)
+
+
 def test_rows_that_see_nothing(B):
     """Empty slots of a batch, negative counts, tables without a page: zeros, and -inf as the log of the sum; a bound of 0."""
     g = gen(9)
@@ -429,6 +466,16 @@ def test_verify_probs(B, V, nb, K):
             for got in _verify(B, p, q, spec, ua, ub, drafted):
                 seen.add(got[0])
     assert len(seen) > 1 or K == 1
+
+
+def test_verify_of_a_large_batch(B):
+    g = np.random.default_rng(8)
+    nb, K, V = 300, 3, 771
+    p, q = _probs(g, (nb, K + 1, V), 1.0), _probs(g, (nb, K, V), 1.0)
+    spec = q.argmax(axis=2)
+    p[np.arange(nb)[:, None], np.arange(K), spec] *= 20
+    got = _verify(B, p, q, spec, g.random((nb, K)).astype(np.float32), g.random(nb).astype(np.float32) * 0.999, g.integers(-2, K + 3, nb))
+    assert {k for k, _ in got} == set(range(K + 1))
 
 
 def test_verify_at_the_edges(B):

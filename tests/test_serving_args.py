@@ -99,7 +99,7 @@ def test_attention_arguments_that_are_refused(b):
     for name in ("kv", "q", "vis", "out", "ws"):
         _refused(b, call(**{name: None}), "null")
     for over, word in [(dict(dtype=3), "dtype"), (dict(heads=3), "multiple"), (dict(heads=0), "multiple"), (dict(heads=2048, q_ld=1 << 18, out_ld=1 << 18), "1024"),
-                       (dict(B=-1), "B in"), (dict(B=70000), "B in"), (dict(T=0), "T in"), (dict(B=65535, T=65535), "2^23"), (dict(most=-1), "max_visible"),
+                       (dict(B=-1), "B in"), (dict(B=70000), "B in"), (dict(T=0), "T in"), (dict(B=65535, T=65535), "2^23"), (dict(T=65535, heads=64, q_ld=4096, out_ld=4096), "KV head"), (dict(most=-1), "max_visible"),
                        (dict(most=257), "block table"), (dict(scale=float("inf")), "scale"), (dict(scale=float("nan")), "scale"), (dict(q_ld=248), "hold"),
                        (dict(out_ld=248), "hold"), (dict(q=P + 8), "16 bytes"), (dict(out=P + 2), "16 bytes"), (dict(ws=P + 4), "16 bytes"),
                        (dict(q_ld=260), "16 bytes"), (dict(out_ld=258), "16 bytes"),
