@@ -165,9 +165,10 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream: Optional[torch.cuda.Stream]) -> int:
+def _stream(stream: Optional[torch.cuda.Stream], device: Optional[int] = None) -> int:
+    """device: the current one, where the caller knows it."""
     if stream is None and _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(torch.cuda.current_device() if device is None else device)
     return (stream or torch.cuda.current_stream()).cuda_stream
 
 
@@ -496,7 +497,7 @@ def ssd_rope(rope: ssd_rope_config, x: torch.Tensor, positions: torch.Tensor, ou
         _bad("ssd_rope: x and out [rows][heads][head_dim], float32 or bfloat16, and positions [rows]")
     _on(dev, torch.int32, positions)
     _check(lib.ssd_rope(rope, x.data_ptr(), _rows(x, dev, dt), _DTYPES[dt], positions.data_ptr(), shape[0], shape[1], shape[2], out.data_ptr(),
-                        _rows(out, dev, dt), _stream(stream)))
+                        _rows(out, dev, dt), _stream(stream, dev)))
 
 
 def ssd_rope_append(rope: ssd_rope_config, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, positions: torch.Tensor, kv: ssd_paged_kv,
@@ -513,7 +514,7 @@ def ssd_rope_append(rope: ssd_rope_config, q: torch.Tensor, k: torch.Tensor, v: 
         _bad("ssd_rope_append: a block table with a row for every sequence, on the queries' GPU")
     _check(lib.ssd_rope_append(rope, kv, q.data_ptr(), _rows(q, dev, dt), k.data_ptr(), _rows(k, dev, dt), v.data_ptr(), _rows(v, dev, dt), _DTYPES[dt],
                                positions.data_ptr(), None if slots is None else slots.data_ptr(), nb, T, hq, q_out.data_ptr(),
-                               _rows(q_out, dev, dt), _stream(stream)))
+                               _rows(q_out, dev, dt), _stream(stream, dev)))
 
 
 def ssd_paged_attention_workspace_bytes(kv: ssd_paged_kv, B: int, T: int, n_q_heads: int, max_visible: int) -> int:
@@ -542,7 +543,7 @@ def ssd_paged_attention(kv: ssd_paged_kv, q: torch.Tensor, visible: torch.Tensor
         _bad("ssd_paged_attention: the workspace is too small")
     _check(lib.ssd_paged_attention(kv, q.data_ptr(), _rows(q, dev, dt), _DTYPES[dt], visible.data_ptr(), nb, T, hq, max_visible,
                                    d ** -0.5 if scale is None else scale, tail, out.data_ptr(), _rows(out, dev, dt),
-                                   None if lse is None else lse.data_ptr(), workspace.data_ptr(), _stream(stream)))
+                                   None if lse is None else lse.data_ptr(), workspace.data_ptr(), _stream(stream, dev)))
 
 
 def ssd_verify_probs_workspace_bytes(B: int, V: int) -> int:
@@ -566,7 +567,7 @@ def ssd_verify_probs(target: torch.Tensor, draft: Optional[torch.Tensor], spec_t
         _bad("ssd_verify_probs: the workspace is too small")
     _check(lib.ssd_verify_probs(target.data_ptr(), V, None if draft is None else draft.data_ptr(), V, spec_tokens.data_ptr(),
                                 None if drafted is None else drafted.data_ptr(), u_accept.data_ptr(), u_bonus.data_ptr(), nb, K1 - 1, V,
-                                accept_len.data_ptr(), bonus.data_ptr(), workspace.data_ptr(), _stream(stream)))
+                                accept_len.data_ptr(), bonus.data_ptr(), workspace.data_ptr(), _stream(stream, dev)))
 
 
 def ssd_ctx_status(ctx: int) -> None:
