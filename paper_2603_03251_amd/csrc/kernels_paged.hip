@@ -509,7 +509,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAttnA
 template <typename TQ, typename TC, int D, int WAVES>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, Parts parts) {
   constexpr int LD = D / 4, NG = WAVES * 64 / LD, E = D / 64, VD = D / 16, LANES = WAVES * 64, PAIRS = 4 / WAVES;
-  constexpr int AHEAD = 4, OWN = WAVES == 4 ? kMaxSplits / LANES : 1;   // splits a lane requests at once, and whose sums it holds
+  constexpr int AHEAD = 4, AHEAD_TAIL = WAVES == 1 ? 4 : 1, OWN = WAVES == 4 ? kMaxSplits / LANES : 1;   // splits a lane requests at once, and whose sums it holds
   static_assert(OWN == 1, "a lane holds one split's maximum and sum");
   __shared__ float w_all[PAIRS][LANES + kMaxTail];
   __shared__ float2 red_ml[4];
@@ -542,7 +542,13 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, Parts 
   const TC* tk = (const TC*)a.tail_k + (row * a.tail_cap * a.n_kv + hk) * D;
   const TC* tv = (const TC*)a.tail_v + (row * a.tail_cap * a.n_kv + hk) * D;
   float* t_s = w_s + LANES;
+  const int d0 = (d4 & 3) * 4 * VD + (d4 >> 2);          // element r of this lane's four is dimension d0 + r VD
+  float tail_v[AHEAD_TAIL][4];
   if (a.tail_len) {
+#pragma unroll
+    for (int i = 0; i < AHEAD_TAIL; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) tail_v[i][r] = Elem<TC>::load(tv + min(gi + i * NG, a.tail_len - 1) * tail_ld + d0 + r * VD);
     float q[E];
     const TQ* qp = (const TQ*)a.q + row * a.q_ld + (int64_t)head * D + lane * E;
 #pragma unroll
@@ -590,9 +596,12 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, Parts 
   for (int i = 0; i < AHEAD; ++i)
     if (gi + i * NG < n) o += part[i] * w_s[gi + i * NG];
   for (int s = gi + AHEAD * NG; s < n; s += NG) o += *(const f32x4*)(po + (int64_t)s * D) * w_s[s];
-  // element r of this lane's four is dimension d0 + r VD
-  const int d0 = (d4 & 3) * 4 * VD + (d4 >> 2);
-  for (int j = gi; j < a.tail_len; j += NG)
+#pragma unroll
+  for (int i = 0; i < AHEAD_TAIL; ++i)
+    if (gi + i * NG < a.tail_len)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[r] = fmaf(t_s[gi + i * NG], tail_v[i][r], o[r]);
+  for (int j = gi + AHEAD_TAIL * NG; j < a.tail_len; j += NG)
 #pragma unroll
     for (int r = 0; r < 4; ++r) o[r] = fmaf(t_s[j], Elem<TC>::load(tv + j * tail_ld + d0 + r * VD), o[r]);
   if constexpr (WAVES == 4) {
