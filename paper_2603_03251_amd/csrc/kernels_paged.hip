@@ -11,7 +11,7 @@
 // Precision: scores, softmax and sums are fp32.  bf16 caches: fp32 queries are three bf16 planes, which is all their 24 bits, and
 // probabilities three too; bf16 queries are their own plane, and probabilities two, 16 bits, where the output keeps 8.
 //
-// What bounds it is the cache's bytes: 64 sequences of 8193 positions, 8 KV heads of 128 dimensions in bf16, 358 us, 6.0 TB/s.  Short ones, the
+// What bounds it is the cache's bytes: 64 sequences of 8193 positions, 8 KV heads of 128 dimensions in bf16, 323 us, 6.6 TB/s.  Short ones, the
 // launches, the chain table entry -> keys -> result, and the join: 6 rows x 4102 positions 12.5 us, 3.4 of them the bytes.  Cached, the first
 // takes 78 us: with every lane loading its own row of the keys' operand it took 148, the cache's lines being asked for 2.5 times as often.
 #include <type_traits>
@@ -89,14 +89,22 @@ __device__ __forceinline__ void split_planes(float x, float y, uint32_t* w, int 
   }
 }
 
+// ONCE: the launch reads every key and value once, and lines need not stay in the caches (no other block comes for them).
+template <bool ONCE>
 __device__ __forceinline__ void load_to_lds(const void* src, uint32_t lds) {     // 16 bytes per lane, to lds + 16 lane
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)(uintptr_t)lds, 16, 0, 0);
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)(uintptr_t)lds, 16, 0,
+                                   ONCE ? 2 : 0);
+}
+template <bool ONCE, typename T>
+__device__ __forceinline__ T load_once(const void* src) {
+  if constexpr (ONCE) return __builtin_nontemporal_load((const T*)src);
+  else return *(const T*)src;
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // PAGES: table entries of a step: 1 where its positions share a page, else one for every 8.
-template <typename TQ, typename TC, int D, int NQ, int PAGES>
+template <typename TQ, typename TC, int D, int NQ, int PAGES, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAttnArgs a, Parts parts) {
   constexpr bool kBf = sizeof(TC) == 2;
   constexpr int KEYS = kBf ? 32 : 16;                    // positions of a wavefront's step
@@ -184,7 +192,7 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAttnA
   auto load_keys = [&](const Place& p) {
 #pragma unroll
     for (int i = 0; i < KL; ++i) {
-      load_to_lds(kbase + off_of(p, i * (64 / CH) / 8) + k_off[i], lds_keys + i * 1024);
+      load_to_lds<ONCE>(kbase + off_of(p, i * (64 / CH) / 8) + k_off[i], lds_keys + i * 1024);
     }
   };
   u32x4 vr[VR];
@@ -194,12 +202,12 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAttnA
     for (int j = 0; j < PER; ++j) {
       const char* p = vbase + off_of(pl, j / 2) + (j & 1) * 4 * pos_bytes + v_off;
       if constexpr (VD * sizeof(TC) == 32) {
-        vr[2 * j] = *(const u32x4*)p;
-        vr[2 * j + 1] = *(const u32x4*)(p + 16);
+        vr[2 * j] = load_once<ONCE, u32x4>(p);
+        vr[2 * j + 1] = load_once<ONCE, u32x4>(p + 16);
       } else if constexpr (VD * sizeof(TC) == 16) {
-        vr[j] = *(const u32x4*)p;
+        vr[j] = load_once<ONCE, u32x4>(p);
       } else {
-        const u32x2 w = *(const u32x2*)p;
+        const u32x2 w = load_once<ONCE, u32x2>(p);
         vr[j / 2][(j & 1) * 2] = w[0];
         vr[j / 2][(j & 1) * 2 + 1] = w[1];
       }
@@ -667,15 +675,22 @@ int launch_d(const PagedAttnArgs& a, hipStream_t s) {
   parts.keys_per_split = p.keys_per_split;
   const dim3 grid(a.n_kv * p.n_splits, p.groups, a.B);
   constexpr int KEYS = sizeof(TC) == 2 ? 32 : 16;
-  auto launch = [&](auto nq) {
+  auto launch = [&](auto nq, auto once) {
     constexpr int NQ = decltype(nq)::value;
-    if (1 << a.page_shift >= KEYS) paged_attention_kernel<TQ, TC, D, NQ, 1><<<grid, 64 * kWaves, 0, s>>>(a, parts);
-    else paged_attention_kernel<TQ, TC, D, NQ, KEYS / 8><<<grid, 64 * kWaves, 0, s>>>(a, parts);
+    constexpr bool ONCE = decltype(once)::value;
+    if (1 << a.page_shift >= KEYS) paged_attention_kernel<TQ, TC, D, NQ, 1, ONCE><<<grid, 64 * kWaves, 0, s>>>(a, parts);
+    else paged_attention_kernel<TQ, TC, D, NQ, KEYS / 8, ONCE><<<grid, 64 * kWaves, 0, s>>>(a, parts);
   };
   if constexpr (kTwoTiles) {
-    if (p.nq == 2) launch(std::integral_constant<int, 2>());
+    if (p.nq == 2) launch(std::integral_constant<int, 2>(), std::false_type());
   }
-  if (p.nq == 1) launch(std::integral_constant<int, 1>());
+  // Lines that no other block comes for need not stay in the caches where the launch reads more than the memory-side cache (256 MB) might keep
+  // for the next one (us, not kept / kept): 64 x 1 row of 64 + 8 heads x 8193 positions of 128 dimensions, 2.1 GB, 322 / 358; 1 x 32768, 134 MB, 27.8 /
+  // 31.0; 16 x 1 row of 16 + 16 heads x 1000, 131 MB, 25.3 / 29.0; but with three sets of inputs in turn 8 x 2 rows of 32 + 8 heads x 4000 of 64
+  // dimensions, 66 MB, 17.8 / 16.6, 1 x 4096, 17 MB, 12.3 / 11.8, and where three blocks read them, 6 rows x 4102, 14.1 / 12.5.
+  const bool once = p.nq == 1 && p.groups == 1 && (double)a.B * a.max_visible * a.n_kv * D * 2 * sizeof(TC) >= 96e6;
+  if (once) launch(std::integral_constant<int, 1>(), std::true_type());
+  else if (p.nq == 1) launch(std::integral_constant<int, 1>(), std::false_type());
   SSD_HIP(hipGetLastError());
   if (p.n_splits > 1 || a.tail_len) {
     const int64_t pairs = (int64_t)a.B * a.T * a.n_q;

@@ -260,6 +260,27 @@ def test_attention_over_long_caches(B, dtype, cache, hq, hkv, D, T, n):
     assert torch.equal(out, again)                    # no order that changes
 
 
+@pytest.mark.parametrize("dtype,cache,page", [(BF16, BF16, 32), (BF16, BF16, 8), (F32, BF16, 64), (F32, F32, 16), (F32, F32, 8), (BF16, F32, 128)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_attention_over_caches_larger_than_the_memory_side_one(B, dtype, cache, page, D):
+    """max_visible sizes the launch: with a bound for which the caches' lines are not kept, rows of few positions and none, garbage behind them."""
+    g, nb, hq, hkv = gen(page + D), 6, 16, 8
+    n = 200_000_000 // (nb * hkv * D * 2 * (2 if cache == BF16 else 4)) // page * page
+    blocks = n // page
+    lens = [0, 1, 700, 33, 256, 3000]
+    c = Cache(B, g, nb, 3000 // page + 1, page, hkv, D, cache)
+    table = np.full((nb, blocks), 2 ** 30, np.int32)
+    table[:, :c.table.shape[1]] = c.table
+    for b, m in enumerate(lens):
+        table[b, -(-m // page):] = -7
+        for j in range(m):
+            c.k[c.place(b, j)] = randn(g, (hkv, D), cache)
+            c.v[c.place(b, j)] = randn(g, (hkv, D), cache)
+    c.table, c.dev_table = table, i32(table)
+    c.kv = B.paged_kv(c.k, c.v, c.dev_table)
+    check_attention(B, c, randn(g, (nb, 1, hq, D), dtype), np.array(lens)[:, None], max_visible=n)
+
+
 @pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("length,capacity", [(0, 3), (1, 1), (5, 7), (70, 256)])
 @pytest.mark.parametrize("D", [64, 128])
