@@ -430,7 +430,7 @@ size_t ssd_paged_attention_workspace_bytes(const ssd_paged_kv* kv, int32_t B, in
 /* Verification (Sec. 2.1) from given probabilities and given random numbers: ssd_verify for callers who filter their distributions
  * (top-p, temperature per request, a grammar) and draw their own numbers.
  *   d_target_probs [B][K+1][V], d_draft_probs [B][K][V] (rows target_ld and draft_ld apart): row i of a sequence = the distribution of the
- *   token after s_1..s_i.  They need not sum to one; what is not a positive finite number counts as zero where a token is drawn.
+ *   token after s_1..s_i.  They need not sum to one; a mass that is not a positive finite number counts as zero.
  *   d_draft_probs NULL: the drafted tokens were certain (a lookup's): q is 1 at s_i and 0 elsewhere.
  *   d_drafted int32 [B] or NULL (all K): sequence b has its first d_drafted[b] tokens only, kept within 0..K (0: its bonus comes from row 0).
  *   d_u_accept [B][K], d_u_bonus [B]: uniform in [0,1).

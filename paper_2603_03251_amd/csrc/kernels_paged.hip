@@ -637,6 +637,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedAttnArgs a, Parts 
 }
 
 constexpr int kWaveSplits = 16;     // splits up to which one wavefront joins a row
+constexpr int kFillSplits = 3;
 constexpr int kSplitStep = 256;     // positions: a step of a block's wavefronts over a bf16 cache, two over an fp32 cache
 
 struct Plan {
@@ -648,6 +649,10 @@ struct Plan {
 // to 2054 of 64 13.8 / 17.8, 1 row of 64 + 8 heads x 32768 31.1 / 37.8).  Two tiles, which read the keys and values once for both, where one each
 // gives two blocks to every unit: 4 x 40 rows of 64 + 8 heads x 8192 122, 156 with one tile; 2 x 300 rows of 32 + 8 heads of 64 dimensions x 2000
 // 38.4, 39.2; not below (6 rows x 4102 15.3, 12.5 with one), and not for fp32 queries, whose planes leave no registers for it.
+// Where there are too many for that but a last round of blocks leaves units idle, up to three splits, if they fill a quarter more and have eight
+// steps to share (us, without / with: 40 x 1 row of 64 + 8 heads x 4000 positions of 128 dimensions 135 / 122, 33 x 1 x 2500 83.5 / 66.7, 4 x 40 x
+// 8192 122 / 110, 10 x 6 fp32 rows of 32 + 8 heads x 6000 of 64 dimensions 53.0 / 42.6; of a smaller gain or of fewer steps the join takes more: 2 x
+// 300 rows x 2000 36.4 / 51.5, 17 x 1 x 700 12.6 / 17.5).
 Plan plan_splits(int B, int T, int n_q, int n_kv, bool two_tiles, int max_visible) {
   Plan p;
   const int tiles = (int)(((int64_t)T * (n_q / n_kv) + 15) / 16);
@@ -658,6 +663,11 @@ Plan plan_splits(int B, int T, int n_q, int n_kv, bool two_tiles, int max_visibl
   int64_t n = units < 256 ? 256 / units : 1;
   n = n < steps ? n : steps;
   n = n < kMaxSplits ? n : kMaxSplits;
+  if (n == 1 && steps >= 8) {
+    auto fill = [&](int64_t x) { return (double)(units * x) / (double)((units * x + 255) / 256); };
+    for (int x = 2; x <= kFillSplits; ++x)
+      if (fill(x) >= 1.25 * fill(1) && fill(x) > fill(n)) n = x;
+  }
   const int each = (int)((steps + n - 1) / n);
   p.keys_per_split = each * kSplitStep;
   p.n_splits = (steps + each - 1) / each;
@@ -715,11 +725,12 @@ size_t paged_attention_workspace(int B, int T, int n_q, int n_kv, int head_dim, 
   return (size_t)B * T * n_q * n * (head_dim + 2) * sizeof(float);
 }
 
-// (splits grow with the positions until there are 256 blocks)
+// (splits grow with the positions until there are 256 blocks; and what 1024 blocks leave idle is less than a quarter)
 size_t paged_attention_workspace_bound(int B, int T, int n_q, int n_kv, int head_dim, int max_visible) {
   const int tiles = (int)(((int64_t)T * (n_q / n_kv) + 15) / 16);
   const int64_t units = (int64_t)B * n_kv * ((tiles + 1) / 2), steps = max_visible / kSplitStep + 1;
   int64_t n = units < 256 ? 256 / units : 1;
+  if (units < 1024 && n < kFillSplits) n = kFillSplits;
   n = n < steps ? n : steps;
   return (size_t)B * T * n_q * n * (head_dim + 2) * sizeof(float);
 }

@@ -282,6 +282,17 @@ def test_attention_over_caches_larger_than_the_memory_side_one(B, dtype, cache, 
 
 
 @pytest.mark.parametrize("dtype,cache", TYPES)
+@pytest.mark.parametrize("nb,T,splits", [(9, 1, 3), (12, 1, 2), (5, 1, 3), (8, 1, 1)])
+def test_attention_of_rows_that_leave_a_last_round_of_blocks(B, dtype, cache, nb, T, splits):
+    """288, 384 and 160 blocks' worth of rows are split to fill the units, 256 are not."""
+    g, hkv, D, n = gen(nb), 32, 64, 2100
+    c = _full_cache(B, g, nb, n, 32, hkv, D, cache)
+    assert B.ssd_paged_attention_workspace_bytes(c.kv, nb, T, hkv, n) == nb * T * hkv * splits * (D + 2) * 4
+    visible = np.array([[[n, 1, 768, 769, 0, 1536, 2099, 1537, 1024][b % 9]] * T for b in range(nb)])
+    check_attention(B, c, randn(g, (nb, T, hkv, D), dtype), visible)
+
+
+@pytest.mark.parametrize("dtype,cache", TYPES)
 @pytest.mark.parametrize("length,capacity", [(0, 3), (1, 1), (5, 7), (70, 256)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_attention_with_tails(B, dtype, cache, length, capacity, D):
