@@ -27,16 +27,32 @@ __device__ __forceinline__ float2 turn_cos_sin(double t) {
   return make_float2(n == 1 || n == 2 ? -ca : ca, n >= 2 ? -sa : sa);
 }
 
-template <typename T, int N>
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
+// STREAM: lines need not stay in the caches.
+template <bool STREAM, typename T>
+__device__ __forceinline__ T get(const T* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  else return *p;
+}
+template <bool STREAM, typename T>
+__device__ __forceinline__ void put(T* p, T v) {
+  if constexpr (STREAM) __builtin_nontemporal_store(v, p);
+  else *p = v;
+}
+
+template <bool STREAM, typename T, int N>
 __device__ __forceinline__ void load_n(const T* p, float* o) {
   if constexpr (N == 1) {
     o[0] = Elem<T>::load(p);
   } else if constexpr (sizeof(T) == 4) {
-    const float4 v = *(const float4*)p;
-    o[0] = v.x; o[1] = v.y; o[2] = v.z; o[3] = v.w;
+    const f32x4 v = get<STREAM>((const f32x4*)p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = v[i];
   } else {
-    const uint4 v = *(const uint4*)p;
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    const u32x4 w = get<STREAM>((const u32x4*)p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       o[2 * i] = __uint_as_float(w[i] << 16);
@@ -44,28 +60,28 @@ __device__ __forceinline__ void load_n(const T* p, float* o) {
     }
   }
 }
-template <typename T, int N>
+template <bool STREAM, typename T, int N>
 __device__ __forceinline__ void store_n(T* p, const float* v) {
   if constexpr (N == 1) {
     Elem<T>::store(p, v[0]);
   } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) *(float4*)(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    for (int i = 0; i < N; i += 4) put<STREAM>((f32x4*)(p + i), (f32x4){v[i], v[i + 1], v[i + 2], v[i + 3]});
   } else {
     typedef __attribute__((ext_vector_type(2))) float f32x2;
     typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
     uint32_t w[N / 2];
 #pragma unroll
     for (int i = 0; i < N / 2; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){v[2 * i], v[2 * i + 1]}, bf16x2));
-    if constexpr (N == 8) *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
-    else *(uint2*)p = make_uint2(w[0], w[1]);
+    if constexpr (N == 8) put<STREAM>((u32x4*)p, (u32x4){w[0], w[1], w[2], w[3]});
+    else put<STREAM>((u32x2*)p, (u32x2){w[0], w[1]});
   }
 }
 
 // One wavefront per (row, group of heads): a lane computes the angle of one pair and passes it on through LDS, then takes 2 VEC
 // elements of a head, the same ones of every head it serves: VEC pairs (with half layout two vectors rot / 2 apart, interleaved
 // two neighbouring ones), or 2 VEC neighbours that are not rotated.  Heads: the queries', the keys', the values'.
-template <typename TI, typename TC, int VEC, int HEADS, bool INTERLEAVED>
+template <typename TI, typename TC, int VEC, int HEADS, bool INTERLEAVED, bool STREAM>
 __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, RopeTurns f) {
   __shared__ float2 cs_all[4][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -90,8 +106,8 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, RopeTurns f) {
     const TI* src = h < a.n_q ? (const TI*)a.q + (int64_t)row * a.q_ld + (int64_t)h * D
                     : h < a.n_q + a.n_kv ? (const TI*)a.k + (int64_t)row * a.k_ld + (int64_t)(h - a.n_q) * D
                                          : (const TI*)a.v + (int64_t)row * a.v_ld + (int64_t)(h - a.n_q - a.n_kv) * D;
-    load_n<TI, VEC>(src + at0, x[it]);
-    load_n<TI, VEC>(src + at1, x[it] + VEC);
+    load_n<STREAM, TI, VEC>(src + at0, x[it]);
+    load_n<STREAM, TI, VEC>(src + at1, x[it] + VEC);
   }
   // where the row's keys and values go: -1 nowhere
   int64_t dst_row = -1;
@@ -133,13 +149,13 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeArgs a, RopeTurns f) {
     }
     if (h < a.n_q) {
       TI* dst = (TI*)a.q_out + (int64_t)row * a.q_out_ld + (int64_t)h * D;
-      store_n<TI, VEC>(dst + at0, v);
-      store_n<TI, VEC>(dst + at1, v + VEC);
+      store_n<STREAM, TI, VEC>(dst + at0, v);
+      store_n<STREAM, TI, VEC>(dst + at1, v + VEC);
     } else if (dst_row >= 0) {
       const bool key = h < a.n_q + a.n_kv;
       TC* dst = (TC*)(key ? a.pool_k : a.pool_v) + dst_row + (int64_t)(h - a.n_q - (key ? 0 : a.n_kv)) * D;
-      store_n<TC, VEC>(dst + at0, v);
-      store_n<TC, VEC>(dst + at1, v + VEC);
+      store_n<STREAM, TC, VEC>(dst + at0, v);
+      store_n<STREAM, TC, VEC>(dst + at1, v + VEC);
     }
   }
 }
@@ -155,8 +171,18 @@ int launch_vec(const RopeArgs& in, const RopeTurns& f, hipStream_t s) {
   constexpr int kMany = VEC == 1 ? 8 : 2;
   a.head_groups = many ? (steps + kMany - 1) / kMany : steps;
   const int64_t blocks = ((int64_t)a.rows * a.head_groups + 3) / 4;
-  if (many) rope_kernel<TI, TC, VEC, kMany, INTERLEAVED><<<(unsigned)blocks, 256, 0, s>>>(a, f);
-  else rope_kernel<TI, TC, VEC, 1, INTERLEAVED><<<(unsigned)blocks, 256, 0, s>>>(a, f);
+  if (!many) {
+    rope_kernel<TI, TC, VEC, 1, INTERLEAVED, false><<<(unsigned)blocks, 256, 0, s>>>(a, f);
+  } else if constexpr (VEC > 1) {
+    // A call that moves more than half of the memory-side cache's 256 MB leaves nothing there that lasts: its lines pass by (us, alone and with a copy of
+    // the queries behind it, without / with: 4093 rows of 64 + 2 x 8 heads of 128 dimensions in bf16, 168 MB, 37.6 / 30.4 and 59.0 / 55.8; 8000 x 72, 295
+    // MB, 56.8 / 50.8 and 127 / 103; not below: 2039 x 72, 75 MB, 14.0 / 14.7 and 26.8 / 30.1).
+    const double bytes = (double)a.rows * a.head_dim * ((a.n_q * 2.0 + a.n_kv * 2.0) * sizeof(TI) + a.n_kv * 2.0 * sizeof(TC));
+    if (bytes >= 128e6) rope_kernel<TI, TC, VEC, kMany, INTERLEAVED, true><<<(unsigned)blocks, 256, 0, s>>>(a, f);
+    else rope_kernel<TI, TC, VEC, kMany, INTERLEAVED, false><<<(unsigned)blocks, 256, 0, s>>>(a, f);
+  } else {
+    rope_kernel<TI, TC, VEC, kMany, INTERLEAVED, false><<<(unsigned)blocks, 256, 0, s>>>(a, f);
+  }
   SSD_HIP(hipGetLastError());
   return SSD_OK;
 }

@@ -76,6 +76,29 @@ def test_rope(B, dtype, heads, D, rot, layout, scaling):
         check_rotated(out, x, positions, freq, layout, 1.25, dtype)
 
 
+@pytest.mark.parametrize("dtype,cache", [(F32, F32), (F32, BF16), (BF16, BF16), (BF16, F32)])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_large_calls_give_the_bits_of_small_ones(B, dtype, cache, layout):
+    """170 MB and more in a call, against calls of 700 rows; in place too."""
+    cfg, _ = _rope(B, 500000.0, 96, layout, "bands")
+    g, T, hq, hkv, D, page = gen(5), 4099 if dtype == BF16 else 2111, 64, 8, 128, 32
+    blocks = -(-T // page)
+    q, k, v = randn(g, (1, T, hq, D), dtype), randn(g, (1, T, hkv, D), dtype), randn(g, (1, T, hkv, D), dtype)
+    pos, table = i32(np.arange(T)[None] + 100000), i32(np.random.default_rng(1).permutation(blocks)[None])
+    slots = i32(np.arange(T)[None])
+    results = []
+    for step in (T, 700):
+        pools = [torch.full((blocks, page, hkv, D), -1.0, dtype=cache, device="cuda") for _ in range(2)]
+        kv, out = B.paged_kv(pools[0], pools[1], table), torch.zeros_like(q)
+        for i in range(0, T, step):
+            part = slice(i, min(i + step, T))
+            B.ssd_rope_append(cfg, q[:, part], k[:, part], v[:, part], pos[:, part].contiguous(), kv, out[:, part], slots=slots[:, part].contiguous())
+        results.append((out, *pools))
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+    B.ssd_rope(cfg, q[0], pos[0], q[0])
+    assert torch.equal(q, results[0][0])
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
 def test_rope_of_views_and_in_place(B, dtype, layout):
