@@ -5,8 +5,8 @@
 // rounding of its result fp32.
 //
 // What bounds it is memory, every element being read once and written once: 2039 rows of 72 heads of 128 dimensions in bf16 14.0 us (a copy of
-// the same tensor 11.8), 4093 rows of 64 query heads with 8 + 8 heads appended 37.9 us, 4.4 TB/s (a copy 33).  Rounding by integer arithmetic and
-// the layout as a value instead of a template argument made them 19.2 and 44.2.
+// the same tensor 11.8), 4093 rows of 64 query heads with 8 + 8 heads appended 30.4 us, 5.5 TB/s (a copy 33), 37.6 of them where lines are kept in the
+// caches; with rounding by integer arithmetic and the layout as a value instead of a template argument 19.2 and 44.2.
 #include "common.h"
 #include "serve.h"
 
@@ -166,7 +166,7 @@ int launch_vec(const RopeArgs& in, const RopeTurns& f, hipStream_t s) {
   const int h_step = 64 / (a.head_dim / (2 * VEC)), n_heads = a.n_q + 2 * a.n_kv;
   const int steps = (n_heads + h_step - 1) / h_step;
   // Two heads to a lane where that leaves enough wavefronts: an angle is then computed half as often (4093 rows of 64 + 2 x 8 heads of 128
-  // dimensions, bf16: 37.9 us, 40.5 with four heads); eight where a lane takes one element of each half only.
+  // dimensions, bf16, lines kept: 37.6 us, 40.5 with four heads); eight where a lane takes one element of each half only.
   const bool many = (int64_t)a.rows * steps >= 8192;
   constexpr int kMany = VEC == 1 ? 8 : 2;
   a.head_groups = many ? (steps + kMany - 1) / kMany : steps;
