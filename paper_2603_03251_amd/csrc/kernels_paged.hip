@@ -89,16 +89,15 @@ __device__ __forceinline__ void split_planes(float x, float y, uint32_t* w, int 
   }
 }
 
+// What is read through a descriptor: `at` is the same for all lanes of a wavefront, which leaves a lane's address a 32-bit offset that does not change from
+// step to step (64-bit addresses of each lane: 8 x 8 fp32 rows of 64 + 8 heads x 3001 fp32 positions 79 us, so 67; 24 branch rows x 8192 17.8, 17.3).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t descriptor(const void* at) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)at, 0, 0xffffffffu, 0x27000);
+}
 // ONCE: the launch reads every key and value once, and lines need not stay in the caches (no other block comes for them).
 template <bool ONCE>
-__device__ __forceinline__ void load_to_lds(const void* src, uint32_t lds) {     // 16 bytes per lane, to lds + 16 lane
-  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)src, (__attribute__((address_space(3))) void*)(uintptr_t)lds, 16, 0,
-                                   ONCE ? 2 : 0);
-}
-template <bool ONCE, typename T>
-__device__ __forceinline__ T load_once(const void* src) {
-  if constexpr (ONCE) return __builtin_nontemporal_load((const T*)src);
-  else return *(const T*)src;
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint32_t off, uint32_t off_all, uint32_t lds) {     // 16 bytes per lane, to lds + 16 lane
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)(uintptr_t)lds, 16, off, off_all, 0, ONCE ? 2 : 0);
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
@@ -175,9 +174,6 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAttnA
     }
     return p;
   };
-  // of the 8 positions from 8 g on
-  auto off_of = [&](const Place& p, int g) { return p.off[g * 8 / SHARE] + (uint32_t)(g * 8 % SHARE) * pos_bytes; };
-
   // Keys go from memory to LDS, a position's row after the other, so that 16 lanes read neighbouring chunks of a row (lanes that loaded
   // their own row of S^T's operand, 16 rows apart, took the cache 2.5 times as long).  Chunk c of position p is at chunk c ^ swizzle(p),
   // which puts the 16 rows that an operand is read from on different banks.
@@ -192,7 +188,9 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAttnA
   auto load_keys = [&](const Place& p) {
 #pragma unroll
     for (int i = 0; i < KL; ++i) {
-      load_to_lds<ONCE>(kbase + off_of(p, i * (64 / CH) / 8) + k_off[i], lds_keys + i * 1024);
+      constexpr int kRows = 64 / CH;                       // of a load
+      const int first = i * kRows / 8 * 8;                 // of the 8 positions that k_off is one of
+      load_to_lds<ONCE>(descriptor(kbase + p.off[first / SHARE]), k_off[i], (uint32_t)(first % SHARE) * pos_bytes, lds_keys + i * 1024);
     }
   };
   u32x4 vr[VR];
@@ -200,14 +198,15 @@ __global__ __launch_bounds__(64 * kWaves) void paged_attention_kernel(PagedAttnA
   auto load_values = [&](const Place& pl) {
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      const char* p = vbase + off_of(pl, j / 2) + (j & 1) * 4 * pos_bytes + v_off;
+      const __amdgpu_buffer_rsrc_t r = descriptor(vbase + pl.off[j * 4 / SHARE]);
+      const uint32_t at = (uint32_t)(j * 4 % SHARE) * pos_bytes;
       if constexpr (VD * sizeof(TC) == 32) {
-        vr[2 * j] = load_once<ONCE, u32x4>(p);
-        vr[2 * j + 1] = load_once<ONCE, u32x4>(p + 16);
+        vr[2 * j] = __builtin_amdgcn_raw_buffer_load_b128(r, v_off, at, ONCE ? 2 : 0);
+        vr[2 * j + 1] = __builtin_amdgcn_raw_buffer_load_b128(r, v_off + 16, at, ONCE ? 2 : 0);
       } else if constexpr (VD * sizeof(TC) == 16) {
-        vr[j] = load_once<ONCE, u32x4>(p);
+        vr[j] = __builtin_amdgcn_raw_buffer_load_b128(r, v_off, at, ONCE ? 2 : 0);
       } else {
-        const u32x2 w = load_once<ONCE, u32x2>(p);
+        const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(r, v_off, at, ONCE ? 2 : 0);
         vr[j / 2][(j & 1) * 2] = w[0];
         vr[j / 2][(j & 1) * 2 + 1] = w[1];
       }
